@@ -7,3 +7,4 @@ from .binding import (  # noqa: F401
     SearchReport, probe_copy, probe_mfma, probe_empty, SpaceReport, expressions, expression_trips, sub_expression, enumerate_space,
     list_candidates3, search_tiles3, tune_tiles3,
 )
+from .cache import KVCache, append_cache, cache_attention, kv_cache, norm_rotate, norm_rotate_backward  # noqa: F401

@@ -14,8 +14,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(ROOT, "_build", "mcf")
 LIB = os.path.join(HERE, "libmcf.so")
-TORCH_EXT = os.path.join(HERE, "_mcf_torch.so")   # extension module of the binding: no kernels, links against libmcf.so
-TORCH_SRC = "mcf_torch.cpp"
+# extension modules of the binding: no kernels, link against libmcf.so
+TORCH_EXTS = {os.path.join(HERE, "_mcf_torch.so"): "mcf_torch.cpp", os.path.join(HERE, "_mcf_cache.so"): "mcf_torch_cache.cpp"}
 
 # -packed-fp32-ops is switched off on purpose: hipcc must not form packed fp32 instructions.
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
@@ -23,19 +23,23 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "
 
 
 def sources():
-    return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".cpp")) and f != TORCH_SRC)
+    return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".cpp")) and f not in TORCH_EXTS.values())
 
 
-def _headers_mtime():
-    hs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".hpp"))]
-    hs.append(os.path.join(ROOT, "include", "mcf.h"))
-    return max(os.path.getmtime(h) for h in hs)
+def _newest(path, seen=None):
+    """The latest modification of a source and of the files that it includes by a path relative to it."""
+    seen = set() if seen is None else seen
+    path = os.path.normpath(path)
+    if path in seen or not os.path.exists(path):
+        return 0.0
+    seen.add(path)
+    names = re.findall(r'^#include "([^"]+)"', open(path).read(), re.M)
+    return max([os.path.getmtime(path)] + [_newest(os.path.join(os.path.dirname(path), n), seen) for n in names])
 
 
-def _compile(src, force, hdr_mtime, extra=()):
+def _compile(src, force, extra=()):
     obj = os.path.join(OBJ_DIR, os.path.basename(src) + ".o")
-    if (not force and os.path.exists(obj) and os.path.getmtime(obj) >= os.path.getmtime(src)
-            and os.path.getmtime(obj) >= hdr_mtime):
+    if not force and os.path.exists(obj) and os.path.getmtime(obj) >= _newest(src):
         return obj
     cmd = (["hipcc"] + HIPCC_FLAGS + list(extra) + (["-x", "hip"] if src.endswith(".cpp") else [])
            + ["-c", src, "-o", obj])
@@ -103,8 +107,8 @@ def _write_resource_table(path):
     return len(rows)
 
 
-def _build_torch_ext():
-    """The extension module the chain calls of the binding go through (host code only)."""
+def _build_torch_ext(ext, src):
+    """An extension module that calls of the binding go through (host code only)."""
     import sysconfig
 
     import torch
@@ -114,27 +118,25 @@ def _build_torch_ext():
            "-isystem", os.path.join(t, "include"), "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
            "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(rocm, "include"),
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
-           os.path.join(CSRC, TORCH_SRC), "-o", TORCH_EXT, LIB, "-L", os.path.join(t, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
+           os.path.join(CSRC, src), "-o", ext, LIB, "-L", os.path.join(t, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
            "-ltorch_hip", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True, cwd=HERE)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("build of " + TORCH_EXT + " failed")
-    return TORCH_EXT
+        raise RuntimeError("build of " + ext + " failed")
 
 
 def build_library(force=True, jobs=8, verbose=False):
     """Compile every source and link libmcf.so.  force=False reuses up-to-date objects."""
     os.makedirs(OBJ_DIR, exist_ok=True)
-    hdr = _headers_mtime()
     srcs = sources()
     kernels = [s for s in srcs if s.endswith(".hip")]
     host = [s for s in srcs if not s.endswith(".hip")]
     with ThreadPoolExecutor(max_workers=jobs) as ex:
-        objs = list(ex.map(lambda s: _compile(s, force, hdr, ["-save-temps=obj"]), kernels))
+        objs = list(ex.map(lambda s: _compile(s, force, ["-save-temps=obj"]), kernels))
     n = _write_resource_table(os.path.join(OBJ_DIR, "mcf_resources.inc"))
     with ThreadPoolExecutor(max_workers=jobs) as ex:
-        objs += list(ex.map(lambda s: _compile(s, True, hdr, ["-I", OBJ_DIR]), host))
+        objs += list(ex.map(lambda s: _compile(s, True, ["-I", OBJ_DIR]), host))
     if verbose:
         print("kernel resource table:", n, "kernels")
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,-soname,libmcf.so", "-o", LIB] + objs
@@ -142,9 +144,10 @@ def build_library(force=True, jobs=8, verbose=False):
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError("link of libmcf.so failed")
-    _build_torch_ext()
+    with ThreadPoolExecutor(max_workers=jobs) as ex:
+        list(ex.map(lambda e: _build_torch_ext(*e), TORCH_EXTS.items()))
     if verbose:
-        print("built", LIB, "from", len(objs), "objects, and", TORCH_EXT)
+        print("built", LIB, "from", len(objs), "objects, and", ", ".join(TORCH_EXTS))
     return LIB
 
 

@@ -1,0 +1,406 @@
+// Attention of few rows over the paged cache of 8 bits: single tokens and a few at once (attend.hpp says how the work is laid out).
+//
+// A block of four waves takes a tile of 16 NB rows and a chunk of tokens, each wave 32 tokens at a time:
+//     S^T = K Q^T   v_mfma 16x16x32, K as its first operand: lane (i, g) = (lane % 16, lane / 16) holds 8 elements of token i
+//     O^T += V^T P^T   the same instruction, contracting 32 tokens: lane (i, g) holds 8 tokens of column i
+// Bound by the cache's bytes: 2 size bytes a token against 4 size flops a row and token, so that up to some 100 rows the
+// matrix instructions wait.  Hence everything goes from memory to registers once, with no LDS between:
+//  - the scores of S^T's result layout (lane: row i, tokens 4g .. 4g + 3 of each 16) are P^T's operand as they are, if the
+//    contraction counts tokens in that order; V is read for the same tokens.
+//  - V's operand wants 8 tokens of one column in a lane, memory has columns side by side: a lane reads size / 16 neighbouring
+//    columns of each of its 8 tokens (whole rows over the 16 lanes) and turns bytes in registers (v_perm); column i of
+//    product j is then column (size / 16) i + j of V, which leaves a lane with neighbouring columns of the result.
+//  - e4m3 -> 16 bit is exact; the scale of K multiplies the scores, that of V the weights, both in fp32.
+//
+// Weights.  bf16: p = 2^(s - m), rounded to bf16 after the factor of V's scale (bf16 has fp32's range).  fp16: V's scale is an
+// exponent like the score's, w = 2^(s + log2 scale - m) <= 2^8 with its own running reference, and the sum of the softmax adds
+// w / scale: the largest weight stands near 1 whatever the scales, where fp16 has all its bits.  Each weight is rounded once.
+// The reference m moves only when a score outgrows it by 2^8.
+//
+// Rows see prefixes of the tokens.  What no row of the tile sees is read as zero; where only some see a token whose value is NaN
+// (0 NaN would be NaN for the others), its column's NaN are counted by a matrix product with who sees them.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "attend.hpp"
+
+namespace mcf {
+namespace attend {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> struct Mma;
+template <> struct Mma<_Float16> {
+    typedef f16x8 v8;
+    static __device__ __forceinline__ f32x4 run(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ uint32_t lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false)); }
+    static __device__ __forceinline__ uint32_t hi(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true)); }
+};
+template <> struct Mma<__bf16> {
+    typedef bf16x8 v8;
+    static __device__ __forceinline__ f32x4 run(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ uint32_t lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false)); }
+    static __device__ __forceinline__ uint32_t hi(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true)); }
+};
+// Eight e4m3 values (in the order of their bytes) as an operand.
+template <typename T> __device__ __forceinline__ typename Mma<T>::v8 widen(uint32_t a, uint32_t b) {
+    const u32x4 w = {Mma<T>::lo(a), Mma<T>::hi(a), Mma<T>::lo(b), Mma<T>::hi(b)};
+    return __builtin_bit_cast(typename Mma<T>::v8, w);
+}
+
+// Byte i of four words as one word, for i = 0 .. 3.
+__device__ __forceinline__ void turn_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3, uint32_t y[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(x1, x0, 0x05010400), b = __builtin_amdgcn_perm(x1, x0, 0x07030602);
+    const uint32_t c = __builtin_amdgcn_perm(x3, x2, 0x05010400), d = __builtin_amdgcn_perm(x3, x2, 0x07030602);
+    y[0] = __builtin_amdgcn_perm(c, a, 0x05040100);
+    y[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
+    y[2] = __builtin_amdgcn_perm(d, b, 0x05040100);
+    y[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
+}
+
+// Columns of V in a lane: 4 (size / 64) of the first 64 (size / 64), and (size % 64) / 16 of the rest.
+template <int D> struct Cols {
+    static constexpr int words = D / 64, rest = D % 64 / 16; // rest: 0, 1 or 2 bytes, in a word of their own
+    static constexpr int regs = words + (rest ? 1 : 0), tiles = 4 * words + rest;
+    // column of product j of lane i
+    static __device__ __forceinline__ int of(int i, int j) { return j < 4 * words ? 4 * words * i + j : 64 * words + rest * i + (j - 4 * words); }
+};
+
+template <int D> struct Step { // 32 tokens of K and V in registers
+    static constexpr bool wide = D % 64 == 0;         // K in 16-byte pieces (two contraction steps each), else 8
+    static constexpr int steps = (D + 31) / 32;
+    uint32_t k[2][2 * steps];
+    uint32_t v[8][Cols<D>::regs];
+    float sk[2], sv[2];
+    float hide[2]; // -inf: these 16 tokens are not there (K, V and K's scale are zeros then)
+};
+
+template <typename T, int D, int NB> struct Rows {
+    typedef typename Mma<T>::v8 v8;
+    typedef Cols<D> C;
+    static constexpr int R = 16 * NB, steps = Step<D>::steps;
+    static constexpr bool f16 = std::is_same<T, _Float16>::value;
+
+    // element of the contraction that lane group g holds first in step s (8 of them; both operands alike)
+    static __device__ __forceinline__ int part(int s, int g) { return Step<D>::wide ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g; }
+
+    static __device__ __forceinline__ void load(const Params &p, int b, int h, int t, int end, Step<D> &x) {
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = t + 16 * j;
+            int id = at < end ? p.seq.table[b * p.seq.table_stride + (at >> p.page_log)] : -1;
+            id = __builtin_amdgcn_readfirstlane(id);
+            const bool there = id >= 0 && id < p.pages;
+            x.hide[j] = there ? 0.f : -INFINITY;
+            if (!there) {
+                x.sk[j] = 0.f;
+                x.sv[j] = 1.f;
+#pragma unroll
+                for (int e = 0; e < 2 * steps; ++e) x.k[j][e] = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < C::regs; ++e) x.v[4 * j + r][e] = 0;
+                continue;
+            }
+            x.sk[j] = p.k_scale[id * p.ks_page + h];
+            x.sv[j] = p.v_scale[id * p.vs_page + h];
+            const int place = at & ((1 << p.page_log) - 1);
+            const uint8_t *k = p.k + id * p.k_page + h * p.k_head + (place + i) * D;
+            if constexpr (Step<D>::wide) {
+#pragma unroll
+                for (int s = 0; s < steps; s += 2) {
+                    const u32x4 w = *(const u32x4 *)(k + part(s, g));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x.k[j][2 * s + e] = w[e];
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < steps; ++s) {
+                    const bool in = D % 32 == 0 || part(s, g) < D;
+                    const u32x2 w = *(const u32x2 *)(k + (in ? part(s, g) : 0));
+                    x.k[j][2 * s] = in ? w[0] : 0;
+                    x.k[j][2 * s + 1] = in ? w[1] : 0;
+                }
+            }
+            const uint8_t *v = p.v + id * p.v_page + h * p.v_head + (place + 4 * g) * D;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t *w = (const uint32_t *)(v + r * D) + C::words * i;
+#pragma unroll
+                for (int e = 0; e < C::words; ++e) x.v[4 * j + r][e] = w[e];
+                if constexpr (C::rest == 1) x.v[4 * j + r][C::words] = v[r * D + 64 * C::words + i];
+                if constexpr (C::rest == 2) x.v[4 * j + r][C::words] = *(const uint16_t *)(v + r * D + 64 * C::words + 2 * i);
+            }
+        }
+    }
+
+    // f(first operand, j) for every product j: 8 tokens of column Cols::of(lane, j)
+    template <typename F> static __device__ __forceinline__ void each_product(const uint32_t v[8][C::regs], F f) {
+#pragma unroll
+        for (int w = 0; w < C::regs; ++w) {
+            uint32_t lo[4], hi[4];
+            turn_bytes(v[0][w], v[1][w], v[2][w], v[3][w], lo);
+            turn_bytes(v[4][w], v[5][w], v[6][w], v[7][w], hi);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * w + e < C::tiles) f(widen<T>(lo[e], hi[e]), 4 * w + e);
+        }
+    }
+
+    struct State {
+        v8 q[NB][steps];
+        f32x4 o[NB][C::tiles];
+        float m[NB], l[NB]; // reference (-inf: nothing seen) and this lane's part of the sum
+        int limit[NB];
+    };
+
+    // 32 tokens from t; HIDE: some of them some row does not see (none sees those from `end` on, all see those below `all`)
+    template <bool HIDE> static __device__ __forceinline__ void step(const Params &p, Step<D> &x, int t, int end, int all, State &st) {
+        const int lane = threadIdx.x & 63, g = lane >> 4;
+        v8 pw[NB];
+        float sv[2], lsv[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            sv[j] = x.sv[j];
+            if constexpr (f16) {
+                sv[j] = fminf(fmaxf(sv[j], 0x1p-60f), 0x1p60f);
+                lsv[j] = __builtin_amdgcn_logf(sv[j]);
+                sv[j] = 1.0f / sv[j];
+            }
+        }
+        f32x4 sc[NB][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) sc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < steps; ++c) {
+                const v8 a = widen<T>(x.k[j][2 * c], x.k[j][2 * c + 1]);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) sc[n][j] = Mma<T>::run(a, st.q[n][c], sc[n][j]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            f32x4 (&s)[2] = sc[n];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float f = p.c * x.sk[j], add = f16 ? lsv[j] + x.hide[j] : x.hide[j];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[j][r] = __builtin_fmaf(s[j][r], f, add);
+                    if (HIDE && t + 16 * j + 4 * g + r >= st.limit[n]) s[j][r] = -INFINITY;
+                }
+            }
+            float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (__any(most > st.m[n] + 8.f)) {
+                const float m = fmaxf(most, st.m[n]);
+                const float by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
+                st.m[n] = m;
+                st.l[n] *= by;
+#pragma unroll
+                for (int c = 0; c < C::tiles; ++c) st.o[n][c] *= by;
+            }
+            const float m = st.m[n] == -INFINITY ? 0.f : st.m[n];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float w = __builtin_amdgcn_exp2f(s[j][r] - m);
+                    st.l[n] = f16 ? __builtin_fmaf(w, sv[j], st.l[n]) : st.l[n] + w;
+                    pw[n][4 * j + r] = (T)(f16 ? w : w * sv[j]);
+                }
+        }
+        if constexpr (HIDE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool seen = t + 16 * (e >> 2) + 4 * g + (e & 3) < end;
+#pragma unroll
+                for (int w = 0; w < C::regs; ++w) x.v[e][w] = seen ? x.v[e][w] : 0;
+            }
+            if (end > all) {
+                bool nan = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int w = 0; w < C::regs; ++w) nan |= (((x.v[e][w] & 0x7f7f7f7f) + 0x01010101) & 0x80808080) != 0;
+                if (__any(nan)) count_nans(x, t, st);
+            }
+        }
+        each_product(x.v, [&](const v8 &a, int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) st.o[n][j] = Mma<T>::run(a, pw[n], st.o[n][j]);
+        });
+    }
+
+    // Takes the NaN out of V and gives them to the rows that see them.
+    static __device__ __forceinline__ void count_nans(Step<D> &x, int t, State &st) {
+        const int g = (threadIdx.x & 63) >> 4;
+        uint32_t ones[8][C::regs];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int w = 0; w < C::regs; ++w) {
+                const uint32_t at = (((x.v[e][w] & 0x7f7f7f7f) + 0x01010101) & 0x80808080) >> 7;
+                ones[e][w] = at * 0x38; // 1 in e4m3
+                x.v[e][w] &= ~(at * 0xff);
+            }
+        v8 sees[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sees[b][e] = t + 16 * (e >> 2) + 4 * g + (e & 3) < st.limit[b] ? (T)1.f : (T)0.f;
+        each_product(ones, [&](const v8 &a, int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const f32x4 n = Mma<T>::run(a, sees[b], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int r = 0; r < 4; ++r) st.o[b][j][r] = n[r] > 0.f ? __builtin_nanf("") : st.o[b][j][r];
+            }
+        });
+    }
+};
+
+template <typename T, int D, int NB> __global__ __launch_bounds__(256) void rows_kernel(const Params p) {
+    typedef Rows<T, D, NB> K;
+    typedef Cols<D> C;
+    constexpr int R = K::R, pitch = D + 4;
+    const uint32_t slot = blockIdx.x / (uint32_t)p.heads;
+    const int h = (int)(blockIdx.x - slot * p.heads);
+    const int chunk = __builtin_amdgcn_readfirstlane(chunk_of<R>(p));
+    int b;
+    uint32_t rest;
+    if (!locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
+            const Sequence s = sequence(p.seq, i);
+            return tiles_of<R>(p, s) * chunks_of(s, chunk);
+        }, &b, &rest)) return;
+    b = __builtin_amdgcn_readfirstlane(b);
+    rest = __builtin_amdgcn_readfirstlane(rest);
+    const Sequence s = sequence(p.seq, b);
+    const uint32_t chunks = chunks_of(s, chunk), tile = rest / chunks, ch = rest - tile * chunks;
+    const int rows = s.rows * p.group - (int)tile * R; // of this tile, of R
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const auto token_of = [&](int r) __attribute__((always_inline)) { return (int)quotient(tile * R + r, p.group_magic, p.group_shift); };
+    const int last = limit_of(p, s, token_of(rows < R ? rows - 1 : R - 1)), all = limit_of(p, s, token_of(0));
+    const int64_t from = (int64_t)ch * chunk;
+    const int end = from + chunk < last ? (int)from + chunk : last; // the tile's tokens in this chunk: from .. end - 1
+
+    typename K::State st;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int r = 16 * n + i;
+        const bool real = r < rows;
+        const int t = token_of(real ? r : 0), head = tile * R + (real ? r : 0) - t * p.group;
+        st.limit[n] = real ? limit_of(p, s, t) : s.seen; // (rows that pad the tile hide nothing)
+        st.m[n] = -INFINITY;
+        st.l[n] = 0.f;
+        const T *q = (const T *)p.q + (int64_t)(s.first + t) * p.qt + (int64_t)(h * p.group + head) * p.qh;
+#pragma unroll
+        for (int c = 0; c < K::steps; ++c) {
+            const bool in = real && (D % 32 == 0 || K::part(c, g) < D);
+            const u32x4 w = *(const u32x4 *)(q + (in ? K::part(c, g) : 0));
+            st.q[n][c] = __builtin_bit_cast(typename K::v8, in ? w : u32x4{0, 0, 0, 0});
+        }
+#pragma unroll
+        for (int c = 0; c < C::tiles; ++c) st.o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int t = (int)(from < end ? from : end) + 32 * wave;
+    const int plain = all < end ? all : end; // every row sees the tokens below
+    if (t + 32 <= plain) {
+        Step<D> x, next;
+        K::load(p, b, h, t, s.seen, x);
+        for (;;) {
+            const int u = t + kStep;
+            const bool more = u + 32 <= plain;
+            if (more) K::load(p, b, h, u, s.seen, next);
+            K::template step<false>(p, x, t, end, all, st);
+            t = u;
+            if (!more) break;
+            x = next;
+        }
+    }
+    for (; t < end; t += kStep) {
+        Step<D> x;
+        K::load(p, b, h, t, s.seen, x);
+        K::template step<true>(p, x, t, end, all, st);
+    }
+
+    // The four waves' parts: each scaled to the largest reference, then summed in the waves' order.
+    __shared__ float ref[4][R], sum[4][R];
+    __shared__ float part[4][16 * pitch];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        st.l[n] += __shfl_xor(st.l[n], 16);
+        st.l[n] += __shfl_xor(st.l[n], 32);
+        if (g == 0) { ref[wave][16 * n + i] = st.m[n]; sum[wave][16 * n + i] = st.l[n]; }
+    }
+    const int64_t place = ((int64_t)slot * p.heads + h) * p.part_rows;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        __syncthreads();
+        const int r = 16 * n + i;
+        const float m = fmaxf(fmaxf(ref[0][r], ref[1][r]), fmaxf(ref[2][r], ref[3][r]));
+        const float by = st.m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[n] - m);
+#pragma unroll
+        for (int c = 0; c < C::tiles; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[wave][i * pitch + C::of(4 * g + e, c)] = st.m[n] == -INFINITY ? 0.f : st.o[n][c][e] * by;
+        __syncthreads();
+        for (int at = threadIdx.x * 4; at < 16 * D; at += 1024) {
+            const int q = at / D, d = at - q * D, row = 16 * n + q;
+            if (row >= rows) continue;
+            f32x4 o = *(const f32x4 *)&part[0][q * pitch + d];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) o += *(const f32x4 *)&part[w][q * pitch + d];
+            const float top = fmaxf(fmaxf(ref[0][row], ref[1][row]), fmaxf(ref[2][row], ref[3][row]));
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) l += ref[w][row] == -INFINITY ? sum[w][row] : sum[w][row] * __builtin_amdgcn_exp2f(ref[w][row] - top); // (nothing seen: 0, or NaN by NaN scores)
+            if (chunks > 1) {
+                *(f32x4 *)(p.part + (place + row) * D + d) = o;
+                if (d == 0) { p.part_ml[2 * (place + row)] = top; p.part_ml[2 * (place + row) + 1] = l; }
+            } else {
+                const float inv = l == 0.f ? 0.f : 1.0f / l; // (0: a row that sees nothing)
+                const int tk = token_of(row), head = tile * R + row - tk * p.group;
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                T4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = (T)(o[e] * inv);
+                *(T4 *)((T *)p.out + (int64_t)(s.first + tk) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
+            }
+        }
+    }
+}
+
+template <typename T> int launch_rows(const Params &p, int size, int row_blocks, unsigned blocks, void *stream) {
+    const auto go = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        if (row_blocks == 1) hipLaunchKernelGGL((rows_kernel<T, D, 1>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+        else if (row_blocks == 2) hipLaunchKernelGGL((rows_kernel<T, D, 2>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+        else if constexpr (D <= 128) hipLaunchKernelGGL((rows_kernel<T, D, 4>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+    };
+    switch (size) {
+    case 64: go(std::integral_constant<int, 64>()); break;
+    case 80: go(std::integral_constant<int, 80>()); break;
+    case 96: go(std::integral_constant<int, 96>()); break;
+    case 128: go(std::integral_constant<int, 128>()); break;
+    case 192: go(std::integral_constant<int, 192>()); break;
+    default: go(std::integral_constant<int, 256>()); break;
+    }
+    return (int)hipGetLastError();
+}
+
+} // namespace
+} // namespace attend
+} // namespace mcf

@@ -1,0 +1,319 @@
+// New keys and values into the paged cache of 8 bits (include/mcf_cache.h): norm and rotation of the keys, the scale of every
+// page and head that tokens go into, rounding to e4m3; and, by further blocks of the same launch, norm and rotation of the
+// queries.
+//
+// A block takes one page and head of K or V: what it needs to know of it (the largest value, the scale so far, the tokens that
+// are held) concerns nobody else, so there are no atomics and the result does not depend on any order.  Its lanes keep
+// the page's new values in registers between the search for the largest and the rounding, so that the inputs are read
+// once.  Bound by memory with prompts (2 bytes in, 1 out an element), by the latency of two dependent loads and a launch with single tokens.
+//
+// Keys are computed in 64 bits: the rounding to e4m3 is a step of 1/16 to 1/8 of a value, and a key that lies next to a border
+// between two steps would otherwise go to either side by the order of the sums, so that the same token appended alone and
+// within a prompt could be held as two values.  A row takes about 150 double operations a lane, behind its loads.
+#include <hip/hip_runtime.h>
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "../../include/mcf_cache.h"
+#include "head_rows.hpp"
+#include "sequences.hpp"
+
+namespace mcf {
+namespace heads {
+namespace {
+
+constexpr float kSmallestScale = 0x1p-100f;
+constexpr int kPasses = 2; // rows of a page that a group of lanes keeps
+
+struct Params {
+    Sequences seq;
+    const void *x[2]; // k, v
+    uint8_t *page[2];
+    float *scale[2];
+    int64_t xt[2], xh[2], page_stride[2], head_stride[2], scale_stride[2];
+    const void *q, *q_weight, *k_weight;
+    void *q_out;
+    int64_t qt, qh, ot, oh;
+    const float *cos, *sin;
+    int64_t table_rows;
+    double eps;
+    float inv_size;
+    int32_t weight_f32, interleaved, size, rotary;
+    int32_t pages, k_heads, page_log;
+    uint32_t cache_blocks;      // slots * heads * 2
+    uint32_t q_items, q_heads;
+    uint32_t heads_magic, q_magic;
+    int32_t heads_shift, q_shift;
+};
+
+// The least power of two that brings x (finite, not negative) to 448 = 1.75 2^8 at most, 2^-100 at least.
+__device__ __forceinline__ float scale_of(float x) {
+    const uint32_t b = __float_as_uint(x);
+    const int e = (int)(b >> 23) - 8 + ((b & 0x7fffff) > 0x600000 ? 1 : 0); // biased
+    return e < 27 ? kSmallestScale : __uint_as_float((uint32_t)e << 23);
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+    x = over_row<32>(x, [](float a, float b) { return fmaxf(a, b); });
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Eight held values at another scale.
+__device__ __forceinline__ void rescale(uint8_t *at, float by) {
+    u32x2 w = *(const u32x2 *)at;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+        w[i] = pack4(lo[0] * by, lo[1] * by, hi[0] * by, hi[1] * by);
+    }
+    *(u32x2 *)at = w;
+}
+
+// The norm and rotation of a key in 64 bits.
+template <typename T, int LPR>
+__device__ __forceinline__ void key_row(const Params &p, const Unit &u, const float wa[8], const float wb[8], const Turn &turn, const Chunk<T> &a, const Chunk<T> &b,
+                                        float va[8], float vb[8]) {
+    double xa[8], xb[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { xa[e] = (double)(float)a.e[e]; xb[e] = (double)(float)b.e[e]; }
+    if (p.k_weight) {
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += xa[e] * xa[e] + xb[e] * xb[e];
+        const double r = 1.0 / sqrt(row_sum<LPR>(sum) / p.size + p.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { xa[e] = xa[e] * r * (double)wa[e]; xb[e] = xb[e] * r * (double)wb[e]; }
+    }
+    if (u.turns) turn.turn<false>(xa, xb, p.interleaved);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { va[e] = (float)xa[e]; vb[e] = (float)xb[e]; }
+}
+
+// One head of one query.
+template <typename T, int LPR> __device__ __forceinline__ void query_row(const Params &p, uint32_t item) {
+    if (item >= p.q_items) return;
+    const uint32_t t = quotient(item, p.q_magic, p.q_shift), h = item - t * p.q_heads;
+    const int b = sequence_of_row(p.seq, (int)t);
+    if (b < 0) return;
+    const Sequence s = sequence(p.seq, b);
+    const Unit u(threadIdx.x % LPR, p.size, p.rotary);
+    const T *x = (const T *)p.q + t * p.qt + h * p.qh;
+    T *out = (T *)p.q_out + t * p.ot + h * p.oh;
+    Chunk<T> a, c;
+    a.bits = c.bits = u32x4{0, 0, 0, 0};
+    if (u.there) { a.bits = *(const u32x4 *)(x + u.a); c.bits = *(const u32x4 *)(x + u.b); }
+    Turn turn;
+    turn.load(p.cos, p.sin, (int64_t)s.length - s.rows + ((int)t - s.first), p.table_rows, p.rotary, u, p.interleaved);
+    float xa[8], xb[8], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { xa[e] = (float)a.e[e]; xb[e] = (float)c.e[e]; sum += xa[e] * xa[e] + xb[e] * xb[e]; }
+    if (p.q_weight) {
+        float wa[8], wb[8];
+        load_weight<T>(p.q_weight, p.weight_f32, u, wa, wb);
+        const float r = 1.0f / sqrtf(row_sum<LPR>(sum) * p.inv_size + (float)p.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { xa[e] = xa[e] * r * wa[e]; xb[e] = xb[e] * r * wb[e]; }
+    }
+    if (u.turns) turn.turn<false>(xa, xb, p.interleaved);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { a.e[e] = (T)xa[e]; c.e[e] = (T)xb[e]; }
+    if (u.there) { *(u32x4 *)(out + u.a) = a.bits; *(u32x4 *)(out + u.b) = c.bits; }
+}
+
+template <typename T, int LPR> __global__ __launch_bounds__(1024) void append_kernel(const Params p) {
+    if (blockIdx.x >= p.cache_blocks) {
+        query_row<T, LPR>(p, (blockIdx.x - p.cache_blocks) * (blockDim.x / LPR) + threadIdx.x / LPR);
+        return;
+    }
+    const int page_size = 1 << p.page_log;
+    const bool is_v = blockIdx.x & 1;
+    const uint32_t sh = blockIdx.x >> 1, slot = quotient(sh, p.heads_magic, p.heads_shift), h = sh - slot * p.k_heads;
+    int b = (int)slot;
+    uint32_t nth = 0;
+    const auto range = [&](const Sequence &s, int &lo, int &hi) __attribute__((always_inline)) { // places that the new tokens have
+        lo = s.length > s.rows ? s.length - s.rows : 0;
+        hi = s.seen;
+    };
+    if (p.seq.starts) {
+        const bool found = locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
+            int lo, hi;
+            range(sequence(p.seq, i), lo, hi);
+            return hi > lo ? ((hi - 1) >> p.page_log) - (lo >> p.page_log) + 1 : 0;
+        }, &b, &nth);
+        if (!found) return;
+    }
+    const Sequence s = sequence(p.seq, b);
+    int lo, hi;
+    range(s, lo, hi);
+    if (s.rows == 0 || hi <= lo) return;
+    const int column = (lo >> p.page_log) + (int)nth;
+    const int id = p.seq.table[b * p.seq.table_stride + column];
+    if (id < 0 || id >= p.pages) return;
+    const int base = column << p.page_log;
+    const int s0 = lo > base ? lo - base : 0, s1 = hi - base < page_size ? hi - base : page_size; // new places of the page
+    float *const scale = p.scale[is_v] + id * p.scale_stride[is_v] + h;
+    uint8_t *const page = p.page[is_v] + id * p.page_stride[is_v] + h * p.head_stride[is_v];
+    const float old = *scale;
+    const Unit u(threadIdx.x % LPR, p.size, p.rotary);
+    const int at_once = blockDim.x / LPR, group = threadIdx.x / LPR;
+    const T *const x = (const T *)p.x[is_v] + h * p.xh[is_v];
+    float va[kPasses][8], vb[kPasses][8], wa[8], wb[8], most = 0.f;
+    if (!is_v && p.k_weight) load_weight<T>(p.k_weight, p.weight_f32, u, wa, wb);
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int place = group + i * at_once;
+        Chunk<T> a, c;
+        a.bits = c.bits = u32x4{0, 0, 0, 0};
+        if (place >= s0 && place < s1 && u.there) {
+            const int64_t t = s.first + (base + place - (s.length - s.rows)); // its row
+            a.bits = *(const u32x4 *)(x + t * p.xt[is_v] + u.a);
+            c.bits = *(const u32x4 *)(x + t * p.xt[is_v] + u.b);
+        }
+        if (!is_v && (p.k_weight || p.rotary)) {
+            Turn turn;
+            turn.load(p.cos, p.sin, base + place, p.table_rows, p.rotary, u, p.interleaved);
+            key_row<T, LPR>(p, u, wa, wb, turn, a, c, va[i], vb[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { va[i][e] = (float)a.e[e]; vb[i][e] = (float)c.e[e]; }
+        }
+        // (the places that are not new have values too where a position is beyond the tables)
+        const bool counts = place >= s0 && place < s1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float *const v[2] = {&va[i][e], &vb[i][e]};
+            for (float *y : v) {
+                const bool finite = fabsf(*y) < INFINITY;
+                if (!finite) *y = __builtin_nanf("");
+                most = fmaxf(most, finite && counts ? fabsf(*y) : 0.f);
+            }
+        }
+    }
+    most = wave_max(most);
+    if (blockDim.x > 64) {
+        __shared__ float part[16];
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+        __syncthreads();
+        for (int w = 0; w < (int)(blockDim.x >> 6); ++w) most = fmaxf(most, part[w]);
+    }
+    float now = scale_of(most);
+    if (s0 > 0) now = fmaxf(now, old);
+    const float inv = 1.0f / now;
+    const bool grows = s0 > 0 && now != old;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int place = group + i * at_once;
+        uint8_t *const to = page + place * p.size;
+        if (!u.there) continue;
+        if (place >= s0 && place < s1) {
+            u32x2 a, c;
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                a[d] = pack4(va[i][4 * d] * inv, va[i][4 * d + 1] * inv, va[i][4 * d + 2] * inv, va[i][4 * d + 3] * inv);
+                c[d] = pack4(vb[i][4 * d] * inv, vb[i][4 * d + 1] * inv, vb[i][4 * d + 2] * inv, vb[i][4 * d + 3] * inv);
+            }
+            *(u32x2 *)(to + u.a) = a;
+            *(u32x2 *)(to + u.b) = c;
+        } else if (grows && place < s0) {
+            rescale(to + u.a, old * inv);
+            rescale(to + u.b, old * inv);
+        }
+    }
+    if (threadIdx.x == 0) *scale = now;
+}
+
+} // namespace
+} // namespace heads
+
+// Checks a call and lays it out; *blocks = 0: nothing to do.  MCF_OK or an error status.
+static int plan_append(const mcf_append_call *c, heads::Params *p, unsigned *blocks, unsigned *threads) {
+    set_last_error("");
+    if (!c) return MCF_EINVAL;
+    if (c->dtype != MCF_F16 && c->dtype != MCF_BF16) return MCF_EUNSUPPORTED;
+    if (c->q_heads < 0 || !(c->eps >= 0.0)) return MCF_EINVAL;
+    const mcf_kv_cache &m = c->cache;
+    int st = check_cache(m);
+    if (st == MCF_OK) st = check_sequences(c->seq, m.page_size);
+    if (st == MCF_OK) st = heads::check_tables(c->rotary, m.size, c->table_rows, c->cos, c->sin);
+    if (st != MCF_OK) return st;
+    for (const void *w : {c->q_weight, c->k_weight})
+        if ((uintptr_t)w % 16 != 0) return MCF_EALIGN;
+    const int64_t tokens = c->seq.tokens;
+    if ((st = heads::check_rows(c->k, 1, tokens, m.heads, m.size, false)) != MCF_OK) return st;
+    if ((st = heads::check_rows(c->v, 1, tokens, m.heads, m.size, false)) != MCF_OK) return st;
+    if ((st = heads::check_rows(c->q, 1, tokens, c->q_heads, m.size, false)) != MCF_OK) return st;
+    if ((st = heads::check_rows(c->q_out, 1, tokens, c->q_heads, m.size, true)) != MCF_OK) return st;
+    if (c->q_heads >= 1 << 20) return MCF_EUNSUPPORTED;
+    // pages that the new tokens of a sequence reach: two more than they fill at most, and no more than there are tokens
+    int64_t slots = tokens / m.page_size + 2 * c->seq.batch;
+    if (slots > tokens) slots = tokens;
+    if (m.pages == 0) slots = 0;
+    const int lanes = heads::row_lanes(m.size);
+    int64_t lanes_needed = m.page_size * lanes / heads::kPasses;
+    *threads = lanes_needed < 64 ? 64u : (unsigned)lanes_needed;
+    const int64_t cache_blocks = slots * m.heads * 2, q_items = tokens * c->q_heads, q_blocks = (q_items + *threads / lanes - 1) / (*threads / lanes);
+    if (slots * m.heads >= 1ll << 30 || q_items >= 1ll << 31 || (cache_blocks + q_blocks) * *threads >= (1ll << 32) - 65536) {
+        set_last_error("too many rows for one call");
+        return MCF_EUNSUPPORTED;
+    }
+    *blocks = (unsigned)(cache_blocks + q_blocks);
+    p->seq = device_sequences(c->seq, m.page_size);
+    p->x[0] = c->k.data; p->x[1] = c->v.data;
+    p->xt[0] = c->k.stride[1]; p->xt[1] = c->v.stride[1];
+    p->xh[0] = c->k.stride[2]; p->xh[1] = c->v.stride[2];
+    p->page[0] = (uint8_t *)m.k; p->page[1] = (uint8_t *)m.v;
+    p->scale[0] = m.k_scale; p->scale[1] = m.v_scale;
+    p->page_stride[0] = m.k_stride[0]; p->page_stride[1] = m.v_stride[0];
+    p->head_stride[0] = m.k_stride[1]; p->head_stride[1] = m.v_stride[1];
+    p->scale_stride[0] = m.k_scale_stride; p->scale_stride[1] = m.v_scale_stride;
+    p->q = c->q.data; p->q_out = c->q_out.data; p->q_weight = c->q_weight; p->k_weight = c->k_weight;
+    p->qt = c->q.stride[1]; p->qh = c->q.stride[2]; p->ot = c->q_out.stride[1]; p->oh = c->q_out.stride[2];
+    p->cos = c->cos; p->sin = c->sin; p->table_rows = c->table_rows;
+    p->eps = c->eps; p->inv_size = 1.0f / (float)m.size;
+    p->weight_f32 = c->weight_f32 != 0; p->interleaved = c->interleaved != 0;
+    p->size = (int32_t)m.size; p->rotary = (int32_t)c->rotary;
+    p->pages = (int32_t)m.pages; p->k_heads = (int32_t)m.heads;
+    p->page_log = m.page_size == 16 ? 4 : m.page_size == 32 ? 5 : m.page_size == 64 ? 6 : 7;
+    p->cache_blocks = (uint32_t)cache_blocks; p->q_items = (uint32_t)q_items; p->q_heads = (uint32_t)c->q_heads;
+    division_magic((uint32_t)m.heads, &p->heads_magic, &p->heads_shift);
+    division_magic((uint32_t)c->q_heads, &p->q_magic, &p->q_shift);
+    return MCF_OK;
+}
+
+int check_append(const mcf_append_call *c) {
+    heads::Params p;
+    unsigned blocks, threads;
+    return plan_append(c, &p, &blocks, &threads);
+}
+
+} // namespace mcf
+
+using namespace mcf;
+
+extern "C" int mcf_cache_append(const mcf_append_call *c, void *stream) {
+    heads::Params p;
+    unsigned blocks, threads;
+    const int st = plan_append(c, &p, &blocks, &threads);
+    if (st != MCF_OK || blocks == 0) return st;
+    const auto run = [&](auto t) {
+        typedef decltype(t) T;
+        const int lanes = heads::row_lanes(p.size);
+        if (lanes == 4) hipLaunchKernelGGL((heads::append_kernel<T, 4>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
+        else if (lanes == 8) hipLaunchKernelGGL((heads::append_kernel<T, 8>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
+        else hipLaunchKernelGGL((heads::append_kernel<T, 16>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
+    };
+    if (c->dtype == MCF_F16) run((_Float16)0);
+    else run((__bf16)0);
+    const hipError_t err = hipGetLastError();
+    if (err == hipSuccess) return MCF_OK;
+    set_last_error(hipGetErrorString(err));
+    return MCF_ELAUNCH;
+}

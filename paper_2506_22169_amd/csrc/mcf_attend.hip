@@ -1,0 +1,175 @@
+// Attention over the paged cache (include/mcf_cache.h): checks, the choice of kernel and split, and the kernel that joins
+// the chunks of a tile.
+#include <hip/hip_runtime.h>
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "attend.hpp"
+#include "head_rows.hpp"
+
+namespace mcf {
+namespace attend {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's chunks, in their order, for the rows of one tile and head.
+template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size) {
+    const uint32_t number = blockIdx.x / (uint32_t)p.heads;
+    const int h = (int)(blockIdx.x - number * p.heads);
+    const int chunk = chunk_of<R>(p);
+    int b;
+    uint32_t tile;
+    if (!locate(number, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
+    const Sequence s = sequence(p.seq, b);
+    const uint32_t chunks = chunks_of(s, chunk);
+    if (chunks == 1) return;
+    // slots before this sequence's
+    uint32_t slot = 0;
+    for (int i = threadIdx.x & 63; i < b; i += 64) {
+        const Sequence o = sequence(p.seq, i);
+        slot += tiles_of<R>(p, o) * chunks_of(o, chunk);
+    }
+    slot = (uint32_t)wave_sum(slot) + tile * chunks;
+    const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
+    const int quads = size / 4;
+    for (int at = threadIdx.x; at < rows * quads; at += 256) {
+        const int row = at / quads, d = 4 * (at - row * quads);
+        const int64_t first = ((int64_t)slot * p.heads + h) * p.part_rows + row, step = (int64_t)p.heads * p.part_rows;
+        float m = -INFINITY;
+        for (uint32_t c = 0; c < chunks; ++c) m = fmaxf(m, p.part_ml[2 * (first + c * step)]);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+        for (uint32_t c = 0; c < chunks; ++c) {
+            const int64_t i = first + c * step;
+            const float mi = p.part_ml[2 * i], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m);
+            l += p.part_ml[2 * i + 1] * by;
+            o += *(const f32x4 *)(p.part + i * size + d) * by;
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        const int r = (int)tile * R + row, t = (int)quotient(r, p.group_magic, p.group_shift), head = r - t * p.group;
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        T4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (T)(o[e] * inv);
+        *(T4 *)((T *)p.out + (int64_t)(s.first + t) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
+    }
+}
+
+struct Plan {
+    Params p;
+    int row_blocks;         // 16 rows each, of a tile
+    unsigned tiles, blocks; // an upper bound of the tiles; 0 blocks: nothing to do
+    int64_t workspace;      // what a split call wants
+};
+
+// Blocks that a call is split up to: four of four waves on every compute unit.
+constexpr int64_t kBlocks = 4 * kComputeUnits;
+
+int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
+    set_last_error("");
+    if (!c) return MCF_EINVAL;
+    if (c->dtype != MCF_F16 && c->dtype != MCF_BF16) return MCF_EUNSUPPORTED;
+    const mcf_kv_cache &m = c->cache;
+    int st = check_cache(m);
+    if (st == MCF_OK) st = check_sequences(c->seq, m.page_size);
+    if (st != MCF_OK) return st;
+    if (!(c->scale - c->scale == 0.f)) return MCF_EINVAL; // NaN, infinity
+    if (c->q_heads < 0 || (c->q_heads > 0 && (m.heads == 0 || c->q_heads % m.heads != 0))) {
+        set_last_error("the heads of the queries are a multiple of the cache's");
+        return MCF_EINVAL;
+    }
+    const int64_t tokens = c->seq.tokens, batch = c->seq.batch;
+    if ((st = heads::check_rows(c->q, 1, tokens, c->q_heads, m.size, false)) != MCF_OK) return st;
+    if ((st = heads::check_rows(c->out, 1, tokens, c->q_heads, m.size, true)) != MCF_OK) return st;
+    o->blocks = 0; o->workspace = 0;
+    if (tokens == 0 || batch == 0 || c->q_heads == 0) return MCF_OK;
+    const int64_t group = c->q_heads / m.heads;
+    if (group > 1 << 16 || tokens * group >= (1ll << 31) - 65536) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; }
+    // the rows that a sequence brings in the mean decide the tile: all of them in one where that is 64 at most
+    const int64_t rows = (tokens * group + batch - 1) / batch;
+    o->row_blocks = rows <= 16 ? 1 : rows <= 32 || m.size > 128 ? 2 : 4;
+    const int R = 16 * o->row_blocks;
+    const int64_t tiles = tokens * group / R + (batch < tokens ? batch : tokens);
+    int64_t slots = kBlocks / m.heads;
+    const bool split = may_split && slots > tiles;
+    if (!split) slots = tiles;
+    if (slots * m.heads >= 1ll << 24) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; } // (2^32 lanes)
+    Params &p = o->p;
+    p.seq = device_sequences(c->seq, m.page_size);
+    if (m.pages == 0) p.seq.capacity = 0;
+    p.q = c->q.data; p.out = c->out.data;
+    p.qt = c->q.stride[1]; p.qh = c->q.stride[2]; p.ot = c->out.stride[1]; p.oh = c->out.stride[2];
+    p.k = (const uint8_t *)m.k; p.v = (const uint8_t *)m.v; p.k_scale = m.k_scale; p.v_scale = m.v_scale;
+    p.k_page = m.k_stride[0]; p.k_head = m.k_stride[1]; p.v_page = m.v_stride[0]; p.v_head = m.v_stride[1];
+    p.ks_page = m.k_scale_stride; p.vs_page = m.v_scale_stride;
+    p.part = p.part_ml = nullptr;
+    p.c = c->scale * 1.44269504088896341f;
+    p.causal = c->causal != 0; p.split = split;
+    p.pages = (int32_t)m.pages; p.heads = (int32_t)m.heads; p.group = (int32_t)group;
+    p.page_log = m.page_size == 16 ? 4 : m.page_size == 32 ? 5 : m.page_size == 64 ? 6 : 7;
+    p.part_rows = c->seq.starts ? R : group < R ? (int)group : R;
+    p.slots = (uint32_t)slots;
+    division_magic((uint32_t)group, &p.group_magic, &p.group_shift);
+    o->tiles = (unsigned)tiles;
+    o->blocks = (unsigned)(slots * m.heads);
+    if (split) o->workspace = slots * m.heads * p.part_rows * (m.size + 2) * 4;
+    return MCF_OK;
+}
+
+} // namespace
+
+int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream) {
+    const auto run = [&](auto t) {
+        typedef decltype(t) T;
+        const dim3 grid(tiles * p.heads), block(256);
+        if (tile_rows == 16) hipLaunchKernelGGL((join_kernel<T, 16>), grid, block, 0, (hipStream_t)stream, p, size);
+        else if (tile_rows == 32) hipLaunchKernelGGL((join_kernel<T, 32>), grid, block, 0, (hipStream_t)stream, p, size);
+        else hipLaunchKernelGGL((join_kernel<T, 64>), grid, block, 0, (hipStream_t)stream, p, size);
+    };
+    if (dtype == MCF_F16) run((_Float16)0);
+    else run((__bf16)0);
+    return (int)hipGetLastError();
+}
+
+} // namespace attend
+
+int check_attention(const mcf_attention_call *c) {
+    attend::Plan l;
+    return attend::plan(c, true, &l);
+}
+
+} // namespace mcf
+
+using namespace mcf;
+
+extern "C" int mcf_cache_attention_workspace(const mcf_attention_call *c, int64_t *bytes) {
+    attend::Plan l;
+    if (!bytes) return MCF_EINVAL;
+    const int st = attend::plan(c, true, &l);
+    *bytes = st == MCF_OK ? l.workspace : 0;
+    return st;
+}
+
+extern "C" int mcf_cache_attention(const mcf_attention_call *c, void *workspace, int64_t workspace_bytes, void *stream) {
+    attend::Plan l;
+    int st = attend::plan(c, true, &l);
+    if (st != MCF_OK || l.blocks == 0) return st;
+    if (l.workspace > 0) {
+        if (!workspace || workspace_bytes < l.workspace) st = attend::plan(c, false, &l);
+        else if ((uintptr_t)workspace % 16 != 0) return MCF_EALIGN;
+        if (st != MCF_OK) return st;
+    }
+    attend::Params &p = l.p;
+    if (l.workspace > 0) {
+        p.part = (float *)workspace;
+        p.part_ml = p.part + (int64_t)l.blocks * p.part_rows * c->cache.size;
+    }
+    const int size = (int)c->cache.size;
+    int err = c->dtype == MCF_F16 ? attend::launch_rows_f16(p, size, l.row_blocks, l.blocks, stream) : attend::launch_rows_bf16(p, size, l.row_blocks, l.blocks, stream);
+    if (err == hipSuccess && l.workspace > 0) err = attend::launch_join(p, c->dtype, size, 16 * l.row_blocks, l.tiles, stream);
+    if (err == hipSuccess) return MCF_OK;
+    set_last_error(hipGetErrorString((hipError_t)err));
+    return MCF_ELAUNCH;
+}

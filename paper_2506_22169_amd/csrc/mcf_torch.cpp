@@ -2,40 +2,9 @@
 // because the marshalling (shapes, strides, the output's allocation, the current stream) is most of
 // what a small chain costs its caller: 15.3 us a call through ctypes, of which the kernel of
 // 1 x [1024,64].[64,128].[128,64] is 4.2 us and the launch 3.
-#include <Python.h>
-
-#include <ATen/ops/empty.h>
-#include <c10/core/DeviceGuard.h>
-#include <c10/hip/HIPCachingAllocator.h>
-#include <c10/hip/HIPGraphsC10Utils.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <stdio.h>
-#include <string.h>
-
-#include "mcf_internal.h"
+#include "torch_call.h"
 
 namespace {
-
-PyObject *g_error = nullptr; // binding.McfError(status, text)
-
-PyObject *fail(int status, const char *text) {
-    PyObject *e = PyObject_CallFunction(g_error, "is", status, text);
-    if (e) {
-        PyErr_SetObject(g_error, e);
-        Py_DECREF(e);
-    }
-    return nullptr;
-}
-
-PyObject *fail_status(int status) {
-    const char *more = mcf_last_error();
-    char text[512];
-    if (*more) snprintf(text, sizeof(text), "%s (%s)", mcf_status_string(status), more);
-    else snprintf(text, sizeof(text), "%s", mcf_status_string(status));
-    return fail(status, text);
-}
 
 // Strides of a [batch, rows, cols] tensor as the C ABI wants them: an empty tensor has no meaningful
 // ones (zeros read as packed), and a dimension of extent <= 1 gets the packed one.
@@ -48,31 +17,6 @@ void strides3(const at::Tensor &t, int64_t s[3]) {
     if (n2 <= 1) s[2] = s[1] == 1 && n1 > 1 ? n1 : 1;
     if (n1 <= 1) s[1] = s[2] == 1 ? n2 : 1;
     if (n0 <= 1) s[0] = 0;
-}
-
-// One element broadcast over a whole tensor: every stride is zero, which the C ABI reads as "packed".
-bool one_element(const at::Tensor &t) {
-    if (t.layout() != at::kStrided || t.numel() <= 1) return false;
-    for (int64_t d = 0; d < t.dim(); ++d)
-        if (t.size(d) > 1 && t.stride(d) != 0) return false;
-    return true;
-}
-
-// The workspace of a call from torch's allocator, for the device of its operands (which need not be the current one) and the
-// stream that the call runs on: given back right after the launches, it is only handed out again to later work of that
-// stream.  While the stream is captured it has to stay with the graph instead.  torch's own capture allocates from the graph's
-// pool, which does that; where someone else captures, memory given back would be used by others between the replays:
-// nullptr then (and in any capture nothing here may end it, so that an allocation may go past the allocator's cache).
-void *workspace(size_t bytes, hipStream_t stream, c10::Device device) {
-    namespace alloc = c10::hip::HIPCachingAllocator;
-    c10::DeviceGuard on(device);
-    if (!mcf::stream_capturing(stream)) return alloc::raw_alloc_with_stream(bytes, stream);
-    c10::hip::HIPStreamCaptureModeGuard allowed(hipStreamCaptureModeRelaxed);
-    void *ws = alloc::raw_alloc_with_stream(bytes, stream);
-    for (const auto &seg : alloc::snapshot().segments)
-        if ((size_t)ws - seg.address < seg.total_size && seg.owner_private_pool_id != c10::MempoolId_t(0, 0)) return ws;
-    alloc::raw_delete(ws);
-    return nullptr;
 }
 
 // Lays a call out and launches it; touches nothing of Python's.
@@ -102,17 +46,6 @@ int run(mcf_call &call, void *stream, c10::Device device) {
     if (ws) c10::hip::HIPCachingAllocator::raw_delete(ws);
     return st;
 }
-
-// The interpreter lock is let go while a call allocates and launches, both of which may wait for the device
-// (and work that is queued may wait for a Python thread); costs 0.1 us a call.
-struct NoGil {
-    PyThreadState *state = PyEval_SaveThread();
-    NoGil() = default;
-    NoGil(const NoGil &) = delete;
-    ~NoGil() { PyEval_RestoreThread(state); }
-};
-
-bool is_tensor(PyObject *o) { return THPVariable_Check(o); }
 
 // chain(kind, scale, causal_offset, A, B, D, F, out, tiles, stream, n_split) -> out
 //   kind: 0 plain, 1 softmax, 2 causal softmax; F: None or the third factor (kind 0 or 1)
@@ -198,13 +131,6 @@ PyObject *chain_entry(PyObject *self, PyObject *const *arg, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     return chain(self, arg, n);
     END_HANDLE_TH_ERRORS
-}
-
-PyObject *set_error(PyObject *, PyObject *type) {
-    Py_INCREF(type);
-    Py_XDECREF(g_error);
-    g_error = type;
-    Py_RETURN_NONE;
 }
 
 PyMethodDef methods[] = {{"chain", (PyCFunction)(void (*)(void))chain_entry, METH_FASTCALL, "one chain call on torch tensors"},
