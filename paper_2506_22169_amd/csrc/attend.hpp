@@ -76,6 +76,8 @@ __device__ __forceinline__ int limit_of(const Params &p, const Sequence &s, int 
 
 int launch_rows_f16(const Params &p, int size, int row_blocks, unsigned blocks, void *stream);  // returns hipError_t as int
 int launch_rows_bf16(const Params &p, int size, int row_blocks, unsigned blocks, void *stream);
+int launch_tiles_f16(const Params &p, int size, int waves, unsigned blocks, void *stream);
+int launch_tiles_bf16(const Params &p, int size, int waves, unsigned blocks, void *stream);
 int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream);
 
 } // namespace attend

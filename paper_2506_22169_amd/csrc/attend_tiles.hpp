@@ -1,0 +1,412 @@
+// Attention of many rows over the paged cache of 8 bits: prompts and pieces of prompts (attend.hpp says how the work is laid out).
+//
+// A block of W waves takes a tile of 32 W rows, each wave 32 of them, and goes over the tokens 64 (size > 128: 32) at a time:
+//     S^T = K Q^T, O^T += V^T P^T   v_mfma 32x32x16; a lane holds one row, so that its softmax needs one exchange (with lane ^ 32),
+//     and S^T's result layout is P^T's operand as it is, with the tokens counted in that order.
+// Bound by the matrix instructions and, next to them, by the vector instructions of the softmax and the LDS reads of their
+// operands.  Therefore
+//  - K and V are widened from e4m3 once for a block (exactly; bf16: with the power of two of V's scale on the way) while they go
+//    from registers to LDS, K as rows, V transposed, so that every operand is one 128-bit read; two tiles of LDS in turn, one
+//    barrier a tile, the loads of the tile after next in flight meanwhile.
+//  - V is transposed by bytes before it is widened: a lane has 4 tokens of 4 neighbouring columns.  Which column is which row of
+//    an operand is free; the order taken (Columns) spreads the writes over the banks and leaves a lane with up to 16
+//    neighbouring columns of the result.
+//  - Padding of 16 bytes a row puts the rows of both on different banks.
+//
+// Weights and what rows do not see: as in attend_rows.hpp, but with the power of two of V's scale in V for bf16 (what the scale is beyond
+// that, in the weights before they are rounded).  A NaN in V that only some
+// rows of the tile see is taken out and its first token noted for its column; rows that see that token get NaN.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "attend.hpp"
+
+namespace mcf {
+namespace attend {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> struct Wide;
+template <> struct Wide<_Float16> {
+    typedef f16x8 v8;
+    typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x16 run(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    template <bool HI> static __device__ __forceinline__ uint32_t two(uint32_t x, float s) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, s, HI));
+    }
+};
+template <> struct Wide<__bf16> {
+    typedef bf16x8 v8;
+    typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x16 run(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    template <bool HI> static __device__ __forceinline__ uint32_t two(uint32_t x, float s) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, HI));
+    }
+};
+
+// Four columns 4c .. 4c + 3 of V (a word of a row) as rows of its operand: 128 columns at a time are four operands, 64 two, then 32
+// and 16 in the last.
+template <int D> struct Columns {
+    static constexpr int operands = (D + 31) / 32;
+    static __device__ __forceinline__ int row(int c, int e) { // of column 4c + e
+        const int part = c >> 5; // 128 columns
+        if (D % 128 == 0 || 128 * part + 128 <= D) return 128 * part + 32 * e + (c & 31);
+        const int base = D / 128 * 128, k = c - base / 4;
+        if (D % 128 >= 64 && k < 16) return base + 32 * (e >> 1) + 2 * k + (e & 1);
+        return base + (D % 128 >= 64 ? 64 : 0) + 4 * (k - (D % 128 >= 64 ? 16 : 0)) + e;
+    }
+};
+
+template <int N> struct Words { uint32_t w[N]; };
+
+template <typename T, int D, int WAVES> struct Tiles {
+    typedef typename Wide<T>::v8 v8;
+    static constexpr bool f16 = std::is_same<T, _Float16>::value;
+    static constexpr int TN = D <= 128 ? 64 : 32, R = 32 * WAVES, threads = 64 * WAVES;
+    static constexpr int blocks = TN / 32, groups = TN / 16, steps = D / 16, operands = Columns<D>::operands;
+    static constexpr int k_pitch = 2 * D + 16, v_pitch = 2 * TN + 16; // bytes
+    static constexpr int k_bytes = TN * k_pitch, v_bytes = 32 * operands * v_pitch;
+    static constexpr int buffer = k_bytes + v_bytes + groups * 16; // and per 16 tokens: factor, addend, 1 / scale of V
+    static constexpr int k_units = TN * D / 16, v_units = TN * D / 16;
+    static constexpr int per_thread = (k_units + threads - 1) / threads;
+    static constexpr int lds = 2 * buffer + D * 4;
+};
+
+template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void tiles_kernel(const Params p) {
+    typedef Tiles<T, D, WAVES> K;
+    typedef typename K::v8 v8;
+    constexpr int TN = K::TN, R = K::R, N = K::per_thread;
+    extern __shared__ __align__(16) uint8_t lds[];
+    int *const first_nan = (int *)(lds + 2 * K::buffer); // [D]: the first token whose value is NaN, of those that not all rows see
+    const uint32_t slot = blockIdx.x / (uint32_t)p.heads;
+    const int h = (int)(blockIdx.x - slot * p.heads);
+    const int chunk = __builtin_amdgcn_readfirstlane(chunk_of<R>(p));
+    int b;
+    uint32_t rest;
+    if (!locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
+            const Sequence s = sequence(p.seq, i);
+            return tiles_of<R>(p, s) * chunks_of(s, chunk);
+        }, &b, &rest)) return;
+    b = __builtin_amdgcn_readfirstlane(b);
+    rest = __builtin_amdgcn_readfirstlane(rest);
+    const Sequence s = sequence(p.seq, b);
+    const uint32_t chunks = chunks_of(s, chunk), at = rest / chunks, ch = rest - at * chunks;
+    const uint32_t tile = tiles_of<R>(p, s) - 1 - at; // the last rows, which see most, first
+    const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i = lane & 31, g = lane >> 5;
+    const auto token_of = [&](int r) __attribute__((always_inline)) { return (int)quotient(tile * R + r, p.group_magic, p.group_shift); };
+    const int all = limit_of(p, s, token_of(0)), last = limit_of(p, s, token_of(rows - 1));
+    const int64_t from64 = (int64_t)ch * chunk;
+    const int end = from64 + chunk < last ? (int)from64 + chunk : last, from = from64 < end ? (int)from64 : end;
+    const int plain = all < end ? all : end; // all rows see the tokens below
+    // this wave's and this lane's rows
+    const int w0 = 32 * wave, row = w0 + i;
+    const bool works = w0 < rows;
+    const int wave_all = works ? limit_of(p, s, token_of(w0)) : 0, wave_last = works ? limit_of(p, s, token_of(w0 + 31 < rows ? w0 + 31 : rows - 1)) : 0;
+    const bool real = row < rows;
+    const int tok = token_of(real ? row : 0), head = (int)(tile * R) + (real ? row : 0) - tok * p.group;
+    const int limit = real ? limit_of(p, s, tok) : s.seen;
+    v8 q[K::steps];
+    {
+        const T *src = (const T *)p.q + (int64_t)(s.first + tok) * p.qt + (int64_t)(h * p.group + head) * p.qh + 8 * g;
+#pragma unroll
+        for (int c = 0; c < K::steps; ++c) {
+            const u32x4 w = *(const u32x4 *)(src + 16 * c);
+            q[c] = __builtin_bit_cast(v8, real ? w : u32x4{0, 0, 0, 0});
+        }
+    }
+    for (int d = tid; d < D; d += K::threads) first_nan[d] = 0x7fffffff;
+
+    // ---- memory to registers to LDS ----
+    const int32_t *const table = p.seq.table + b * p.seq.table_stride;
+    const auto page_of = [&](int t) __attribute__((always_inline)) { // of token t, -1: not there
+        const int id = t < s.seen ? table[t >> p.page_log] : -1;
+        return id < p.pages ? id : -1;
+    };
+    const int in_page = (1 << p.page_log) - 1;
+    int k_id[N], v_id[N], g_id = -1; // pages of the tile to load next
+    u32x4 kw[N];                     // 16 elements of a token
+    uint32_t vw[N][4];               // 4 columns of 4 tokens
+    float ks = 0.f, vs = 1.f, v_scale[N];
+    bool there = false;
+    const auto look_up = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int unit = tid + u * K::threads;
+            k_id[u] = unit < K::k_units ? page_of(t0 + unit / (D / 16)) : -1;
+            v_id[u] = unit < K::v_units ? page_of(t0 + unit / (D / 4) * 4) : -1;
+        }
+        if (tid < K::groups) g_id = page_of(t0 + 16 * tid);
+    };
+    const auto load = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int unit = tid + u * K::threads;
+            kw[u] = u32x4{0, 0, 0, 0};
+            if (k_id[u] >= 0) {
+                const int token = unit / (D / 16), c = unit % (D / 16);
+                kw[u] = *(const u32x4 *)(p.k + k_id[u] * p.k_page + h * p.k_head + ((t0 + token) & in_page) * D + 16 * c);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vw[u][r] = 0;
+            v_scale[u] = 1.f;
+            if (v_id[u] >= 0) {
+                const int token = unit / (D / 4) * 4, c = unit % (D / 4);
+                const uint8_t *v = p.v + v_id[u] * p.v_page + h * p.v_head + ((t0 + token) & in_page) * D + 4 * c;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vw[u][r] = *(const uint32_t *)(v + r * D);
+                if (!K::f16) v_scale[u] = p.v_scale[v_id[u] * p.vs_page + h];
+            }
+        }
+        if (tid < K::groups) {
+            there = g_id >= 0;
+            ks = there ? p.k_scale[g_id * p.ks_page + h] : 0.f;
+            vs = there ? p.v_scale[g_id * p.vs_page + h] : 1.f;
+        }
+    };
+    const auto store = [&](uint8_t *buf, int t0) __attribute__((always_inline)) {
+        const bool hides = t0 + TN > plain;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int unit = tid + u * K::threads;
+            if (K::k_units % K::threads != 0 && unit >= K::k_units) continue;
+            {
+                const int token = unit / (D / 16), c = unit % (D / 16);
+                u32x4 lo, hi;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    lo[2 * e] = Wide<T>::template two<false>(kw[u][e], 1.f);
+                    lo[2 * e + 1] = Wide<T>::template two<true>(kw[u][e], 1.f);
+                    hi[2 * e] = Wide<T>::template two<false>(kw[u][2 + e], 1.f);
+                    hi[2 * e + 1] = Wide<T>::template two<true>(kw[u][2 + e], 1.f);
+                }
+                *(u32x4 *)(buf + token * K::k_pitch + 32 * c) = lo;
+                *(u32x4 *)(buf + token * K::k_pitch + 32 * c + 16) = hi;
+            }
+            const int token = unit / (D / 4) * 4, c = unit % (D / 4);
+            if (hides) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t &x = vw[u][r];
+                    if (t0 + token + r >= end) x = 0;
+                    if (end <= all) continue; // (what is left all rows see)
+                    const uint32_t nan = (((x & 0x7f7f7f7f) + 0x01010101) & 0x80808080) >> 7;
+                    if (nan) {
+                        x &= ~(nan * 0xff);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (nan >> (8 * e) & 1) atomicMin(first_nan + 4 * c + e, t0 + token + r);
+                    }
+                }
+            }
+            // bytes of a column together
+            uint32_t y[4];
+            const uint32_t a0 = __builtin_amdgcn_perm(vw[u][1], vw[u][0], 0x05010400), a1 = __builtin_amdgcn_perm(vw[u][1], vw[u][0], 0x07030602);
+            const uint32_t a2 = __builtin_amdgcn_perm(vw[u][3], vw[u][2], 0x05010400), a3 = __builtin_amdgcn_perm(vw[u][3], vw[u][2], 0x07030602);
+            y[0] = __builtin_amdgcn_perm(a2, a0, 0x05040100);
+            y[1] = __builtin_amdgcn_perm(a2, a0, 0x07060302);
+            y[2] = __builtin_amdgcn_perm(a3, a1, 0x05040100);
+            y[3] = __builtin_amdgcn_perm(a3, a1, 0x07060302);
+            // tokens 4t of 16 stand at 8 (t % 2) + 4 (t / 2), the order of S^T's result
+            const int t = token >> 2, place = (token & ~15) + 8 * (t & 1) + 4 * ((t >> 1) & 1);
+            uint8_t *const to = buf + K::k_bytes + 2 * place;
+            const float sv = K::f16 ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
+        }
+        if (tid < K::groups) {
+            f32x4 x = {p.c * ks, there ? 0.f : -INFINITY, 1.f, 0.f};
+            if (K::f16) {
+                const float v = fminf(fmaxf(vs, 0x1p-60f), 0x1p60f);
+                x[1] += __builtin_amdgcn_logf(v);
+                x[2] = 1.0f / v;
+            } else { // what V's scale is beyond its power of two
+                x[2] = __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
+            }
+            *(f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * tid) = x;
+        }
+    };
+
+    // ---- a tile ----
+    f32x16 o[K::operands];
+#pragma unroll
+    for (int c = 0; c < K::operands; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][r] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const auto compute = [&](const uint8_t *buf, int t0) __attribute__((always_inline)) {
+        f32x16 sc[K::blocks];
+        const uint8_t *kp = buf + i * K::k_pitch + 16 * g;
+#pragma unroll
+        for (int j = 0; j < K::blocks; ++j) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[j][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < K::steps; ++c) sc[j] = Wide<T>::run(*(const v8 *)(kp + 32 * j * K::k_pitch + 32 * c), q[c], sc[j]);
+        }
+        f32x4 par[K::groups];
+#pragma unroll
+        for (int k = 0; k < K::groups; ++k) par[k] = *(const f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * k);
+        float most = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < K::blocks; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[j][r] = __builtin_fmaf(sc[j][r], par[2 * j + (r >> 3)][0], par[2 * j + (r >> 3)][1]);
+        if (t0 + TN > wave_all) {
+            const int room = limit - t0 - 4 * g;
+#pragma unroll
+            for (int j = 0; j < K::blocks; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sc[j][r] = 32 * j + 8 * (r >> 2) + (r & 3) < room ? sc[j][r] : -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < K::blocks; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) most = fmaxf(fmaxf(sc[j][r], sc[j][r + 1]), most);
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (__any(most > m + 8.f)) {
+            const float top = fmaxf(most, m), by = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= by;
+#pragma unroll
+            for (int c = 0; c < K::operands; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[c][r] *= by;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        v8 pw[2 * K::blocks];
+#pragma unroll
+        for (int j = 0; j < K::blocks; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float w = __builtin_amdgcn_exp2f(sc[j][r] - ref);
+                l = K::f16 ? __builtin_fmaf(w, par[2 * j + (r >> 3)][2], l) : l + w;
+                sc[j][r] = w;
+            }
+        if constexpr (!K::f16) {
+            float over = 0.f;
+#pragma unroll
+            for (int k = 0; k < K::groups; ++k) over += par[k][2] - 1.f;
+            if (__builtin_amdgcn_readfirstlane(__float_as_uint(over)) != 0) {
+#pragma unroll
+                for (int j = 0; j < K::blocks; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sc[j][r] *= par[2 * j + (r >> 3)][2];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < K::blocks; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) pw[2 * j + (r >> 3)][r & 7] = (T)sc[j][r];
+        const uint8_t *vp = buf + K::k_bytes + i * K::v_pitch + 16 * g;
+#pragma unroll
+        for (int c = 0; c < K::operands; ++c)
+#pragma unroll
+            for (int k = 0; k < K::groups; ++k) o[c] = Wide<T>::run(*(const v8 *)(vp + 32 * c * K::v_pitch + 32 * k), pw[k], o[c]);
+    };
+
+    if (from < end) {
+        look_up(from);
+        load(from);
+        look_up(from + TN);
+        __syncthreads(); // (first_nan)
+        store(lds, from);
+        load(from + TN);
+        look_up(from + 2 * TN);
+        __syncthreads();
+        int turn = 0;
+        for (int t0 = from; t0 < end; t0 += TN) {
+            if (t0 < wave_last) compute(lds + turn * K::buffer, t0);
+            turn ^= 1;
+            if (t0 + TN < end) {
+                store(lds + turn * K::buffer, t0 + TN);
+                load(t0 + 2 * TN);
+                look_up(t0 + 3 * TN);
+            }
+            __syncthreads();
+        }
+    } else {
+        __syncthreads();
+    }
+
+    // ---- the result ----
+    l += __shfl_xor(l, 32);
+    if (!real) return;
+    const bool whole = chunks == 1;
+    const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.0f / l;
+    const int64_t place = ((int64_t)(slot - rest + tile * chunks + ch) * p.heads + h) * p.part_rows + row; // (slots count tiles upwards)
+    if (!whole && g == 0) { p.part_ml[2 * place] = m; p.part_ml[2 * place + 1] = l; }
+    T *const out = (T *)p.out + (int64_t)(s.first + tok) * p.ot + (int64_t)(h * p.group + head) * p.oh;
+    // n neighbouring columns from d, their products o[c0 + x / per] at register r0 + x % per
+    const auto put = [&](int d, auto count, auto value) __attribute__((always_inline)) {
+        constexpr int n = decltype(count)::value;
+        typedef T Tn __attribute__((ext_vector_type(n)));
+        float x[n];
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+            x[e] = value(e) * inv;
+            if (end > all && first_nan[d + e] < limit) x[e] = __builtin_nanf("");
+        }
+        if (whole) {
+            Tn y;
+#pragma unroll
+            for (int e = 0; e < n; ++e) y[e] = (T)x[e];
+            *(Tn *)(out + d) = y;
+        } else {
+#pragma unroll
+            for (int e = 0; e < n; e += 4) *(f32x4 *)(p.part + place * D + d + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        }
+    };
+#pragma unroll
+    for (int a = 0; a < 4; ++a) { // rows 8a + 4g + 0 .. 3 of the operands
+#pragma unroll
+        for (int c = 0; c < D / 128; ++c)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                put(128 * c + 32 * a + 16 * g + 8 * half, std::integral_constant<int, 8>(), [&](int e) __attribute__((always_inline)) { return o[4 * c + (e & 3)][4 * a + 2 * half + (e >> 2)]; });
+        constexpr int c64 = D / 128 * 4, d64 = D / 128 * 128;
+        if constexpr (D % 128 >= 64)
+            put(d64 + 16 * a + 8 * g, std::integral_constant<int, 8>(), [&](int e) __attribute__((always_inline)) { return o[c64 + ((e & 3) >> 1)][4 * a + 2 * (e >> 2) + (e & 1)]; });
+        constexpr int c32 = c64 + (D % 128 >= 64 ? 2 : 0), d32 = d64 + (D % 128 >= 64 ? 64 : 0);
+        if constexpr (D % 64 >= 16)
+            if (8 * a + 4 * g < (D % 64) / 4 * 4 && 8 * a + 4 * g < D % 64)
+                put(d32 + 8 * a + 4 * g, std::integral_constant<int, 4>(), [&](int e) __attribute__((always_inline)) { return o[c32][4 * a + e]; });
+    }
+}
+
+template <typename T, int D, int WAVES> int launch_tile(const Params &p, unsigned blocks, void *stream) {
+    typedef Tiles<T, D, WAVES> K;
+    static const hipError_t set = hipFuncSetAttribute((const void *)tiles_kernel<T, D, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, K::lds);
+    if (set != hipSuccess) return (int)set;
+    hipLaunchKernelGGL((tiles_kernel<T, D, WAVES>), dim3(blocks), dim3(K::threads), K::lds, (hipStream_t)stream, p);
+    return (int)hipGetLastError();
+}
+
+template <typename T> int launch_tiles(const Params &p, int size, int waves, unsigned blocks, void *stream) {
+    const auto go = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        return waves == 4 ? launch_tile<T, D, 4>(p, blocks, stream) : launch_tile<T, D, 8>(p, blocks, stream);
+    };
+    switch (size) {
+    case 64: return go(std::integral_constant<int, 64>());
+    case 80: return go(std::integral_constant<int, 80>());
+    case 96: return go(std::integral_constant<int, 96>());
+    case 128: return go(std::integral_constant<int, 128>());
+    case 192: return go(std::integral_constant<int, 192>());
+    default: return go(std::integral_constant<int, 256>());
+    }
+}
+
+} // namespace
+} // namespace attend
+} // namespace mcf

@@ -14,52 +14,62 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's chunks, in their order, for the rows of one tile and head.
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's chunks, for one row of a tile and head.  A block's lanes take
+// four elements of every (256 / (size / 4))-th chunk each; their sums are added in that order.
 template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size) {
-    const uint32_t number = blockIdx.x / (uint32_t)p.heads;
-    const int h = (int)(blockIdx.x - number * p.heads);
+    const uint32_t row_of = blockIdx.x / (uint32_t)p.part_rows, number = row_of / (uint32_t)p.heads;
+    const int row = (int)(blockIdx.x - row_of * p.part_rows), h = (int)(row_of - number * p.heads);
     const int chunk = chunk_of<R>(p);
     int b;
     uint32_t tile;
     if (!locate(number, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
     const Sequence s = sequence(p.seq, b);
-    const uint32_t chunks = chunks_of(s, chunk);
-    if (chunks == 1) return;
-    // slots before this sequence's
-    uint32_t slot = 0;
+    const int chunks = (int)chunks_of(s, chunk);
+    if (chunks == 1 || s.rows * p.group - (int)tile * R <= row) return;
+    uint32_t slot = 0; // slots before this sequence's
     for (int i = threadIdx.x & 63; i < b; i += 64) {
         const Sequence o = sequence(p.seq, i);
         slot += tiles_of<R>(p, o) * chunks_of(o, chunk);
     }
     slot = (uint32_t)wave_sum(slot) + tile * chunks;
-    const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
-    const int quads = size / 4;
-    for (int at = threadIdx.x; at < rows * quads; at += 256) {
-        const int row = at / quads, d = 4 * (at - row * quads);
-        const int64_t first = ((int64_t)slot * p.heads + h) * p.part_rows + row, step = (int64_t)p.heads * p.part_rows;
-        float m = -INFINITY;
-        for (uint32_t c = 0; c < chunks; ++c) m = fmaxf(m, p.part_ml[2 * (first + c * step)]);
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        float l = 0.f;
-        for (uint32_t c = 0; c < chunks; ++c) {
+    const int64_t first = ((int64_t)slot * p.heads + h) * p.part_rows + row, step = (int64_t)p.heads * p.part_rows;
+    float m = -INFINITY;
+    for (int c = threadIdx.x & 63; c < chunks; c += 64) m = fmaxf(m, p.part_ml[2 * (first + c * step)]);
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    const int quads = size / 4, slices = 256 / quads, slice = threadIdx.x / quads, d = 4 * (threadIdx.x - slice * quads);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    if (slice < slices) {
+#pragma unroll 4
+        for (int c = slice; c < chunks; c += slices) {
             const int64_t i = first + c * step;
-            const float mi = p.part_ml[2 * i], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m);
+            const float mi = p.part_ml[2 * i], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m); // (nothing seen: zeros, or NaN)
             l += p.part_ml[2 * i + 1] * by;
             o += *(const f32x4 *)(p.part + i * size + d) * by;
         }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const int r = (int)tile * R + row, t = (int)quotient(r, p.group_magic, p.group_shift), head = r - t * p.group;
-        typedef T T4 __attribute__((ext_vector_type(4)));
-        T4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (T)(o[e] * inv);
-        *(T4 *)((T *)p.out + (int64_t)(s.first + t) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
     }
+    __shared__ f32x4 part[256];
+    __shared__ float sum[256];
+    part[threadIdx.x] = o;
+    sum[threadIdx.x] = l;
+    __syncthreads();
+    if (slice != 0) return;
+    for (int i = 1; i < slices; ++i) {
+        o += part[threadIdx.x + i * quads];
+        l += sum[threadIdx.x + i * quads];
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const int r = (int)tile * R + row, t = (int)quotient(r, p.group_magic, p.group_shift), head = r - t * p.group;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (T)(o[e] * inv);
+    *(T4 *)((T *)p.out + (int64_t)(s.first + t) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
 }
 
 struct Plan {
     Params p;
-    int row_blocks;         // 16 rows each, of a tile
+    int tile_rows;          // 16, 32, 64: attend_rows.hpp; 128, 256: attend_tiles.hpp
     unsigned tiles, blocks; // an upper bound of the tiles; 0 blocks: nothing to do
     int64_t workspace;      // what a split call wants
 };
@@ -87,15 +97,14 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     if (tokens == 0 || batch == 0 || c->q_heads == 0) return MCF_OK;
     const int64_t group = c->q_heads / m.heads;
     if (group > 1 << 16 || tokens * group >= (1ll << 31) - 65536) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; }
-    // the rows that a sequence brings in the mean decide the tile: all of them in one where that is 64 at most
+    // the rows that a sequence brings in the mean decide the tile
     const int64_t rows = (tokens * group + batch - 1) / batch;
-    o->row_blocks = rows <= 16 ? 1 : rows <= 32 || m.size > 128 ? 2 : 4;
-    const int R = 16 * o->row_blocks;
+    const int R = o->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && m.size <= 128 ? 64 : rows <= 128 ? 128 : 256;
     const int64_t tiles = tokens * group / R + (batch < tokens ? batch : tokens);
     int64_t slots = kBlocks / m.heads;
     const bool split = may_split && slots > tiles;
     if (!split) slots = tiles;
-    if (slots * m.heads >= 1ll << 24) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; } // (2^32 lanes)
+    if (slots * m.heads >= 1ll << 23) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; } // (2^32 lanes)
     Params &p = o->p;
     p.seq = device_sequences(c->seq, m.page_size);
     if (m.pages == 0) p.seq.capacity = 0;
@@ -123,10 +132,12 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
 int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream) {
     const auto run = [&](auto t) {
         typedef decltype(t) T;
-        const dim3 grid(tiles * p.heads), block(256);
+        const dim3 grid(tiles * p.heads * p.part_rows), block(256);
         if (tile_rows == 16) hipLaunchKernelGGL((join_kernel<T, 16>), grid, block, 0, (hipStream_t)stream, p, size);
         else if (tile_rows == 32) hipLaunchKernelGGL((join_kernel<T, 32>), grid, block, 0, (hipStream_t)stream, p, size);
-        else hipLaunchKernelGGL((join_kernel<T, 64>), grid, block, 0, (hipStream_t)stream, p, size);
+        else if (tile_rows == 64) hipLaunchKernelGGL((join_kernel<T, 64>), grid, block, 0, (hipStream_t)stream, p, size);
+        else if (tile_rows == 128) hipLaunchKernelGGL((join_kernel<T, 128>), grid, block, 0, (hipStream_t)stream, p, size);
+        else hipLaunchKernelGGL((join_kernel<T, 256>), grid, block, 0, (hipStream_t)stream, p, size);
     };
     if (dtype == MCF_F16) run((_Float16)0);
     else run((__bf16)0);
@@ -167,8 +178,11 @@ extern "C" int mcf_cache_attention(const mcf_attention_call *c, void *workspace,
         p.part_ml = p.part + (int64_t)l.blocks * p.part_rows * c->cache.size;
     }
     const int size = (int)c->cache.size;
-    int err = c->dtype == MCF_F16 ? attend::launch_rows_f16(p, size, l.row_blocks, l.blocks, stream) : attend::launch_rows_bf16(p, size, l.row_blocks, l.blocks, stream);
-    if (err == hipSuccess && l.workspace > 0) err = attend::launch_join(p, c->dtype, size, 16 * l.row_blocks, l.tiles, stream);
+    const bool f16 = c->dtype == MCF_F16;
+    int err;
+    if (l.tile_rows <= 64) err = (f16 ? attend::launch_rows_f16 : attend::launch_rows_bf16)(p, size, l.tile_rows / 16, l.blocks, stream);
+    else err = (f16 ? attend::launch_tiles_f16 : attend::launch_tiles_bf16)(p, size, l.tile_rows / 32, l.blocks, stream);
+    if (err == hipSuccess && l.workspace > 0) err = attend::launch_join(p, c->dtype, size, l.tile_rows, l.tiles, stream);
     if (err == hipSuccess) return MCF_OK;
     set_last_error(hipGetErrorString((hipError_t)err));
     return MCF_ELAUNCH;
