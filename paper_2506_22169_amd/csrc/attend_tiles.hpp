@@ -66,7 +66,8 @@ template <int D> struct Columns {
     }
 };
 
-template <int N> struct Words { uint32_t w[N]; };
+// A barrier for what is in LDS: global loads stay in flight over it (__syncthreads() waits for them).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <typename T, int D, int WAVES> struct Tiles {
     typedef typename Wide<T>::v8 v8;
@@ -128,71 +129,74 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
 
     // ---- memory to registers to LDS ----
     const int32_t *const table = p.seq.table + b * p.seq.table_stride;
-    const auto page_of = [&](int t) __attribute__((always_inline)) { // of token t, -1: not there
-        const int id = t < s.seen ? table[t >> p.page_log] : -1;
-        return id < p.pages ? id : -1;
-    };
     const int in_page = (1 << p.page_log) - 1;
-    int k_id[N], v_id[N], g_id = -1; // pages of the tile to load next
-    u32x4 kw[N];                     // 16 elements of a token
-    uint32_t vw[N][4];               // 4 columns of 4 tokens
+    int k_id[N], v_id[N], g_id = 0; // table entries for the tile to load next
+    bool k_there[N], v_there[N], there = false;
+    u32x4 kw[N];                    // 16 elements of a token
+    uint32_t vw[N][4];              // 4 columns of 4 tokens
     float ks = 0.f, vs = 1.f, v_scale[N];
-    bool there = false;
+    int k_token[N], v_token[N], k_at[N], v_at[N]; // this lane's: tokens of a tile, offsets in a token
+#pragma unroll
+    for (int u = 0; u < N; ++u) { // (lanes beyond the last unit load that one again and store nothing)
+        const int unit = K::k_units % K::threads != 0 && tid + u * K::threads >= K::k_units ? K::k_units - 1 : tid + u * K::threads;
+        k_token[u] = unit / (D / 16);
+        k_at[u] = unit % (D / 16) * 16;
+        v_token[u] = unit / (D / 4) * 4;
+        v_at[u] = unit % (D / 4) * 4;
+    }
+    // Nothing here waits for a load: entries are looked at when the loads of their tile are issued, a tile later, and what is not there
+    // is read from the first page and dropped when it is stored.
+    const auto entry = [&](int t) __attribute__((always_inline)) { return table[(t < s.seen ? t : s.seen - 1) >> p.page_log]; };
+    const auto valid = [&](int t, int id) __attribute__((always_inline)) { return t < s.seen && id >= 0 && id < p.pages; };
     const auto look_up = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int unit = tid + u * K::threads;
-            k_id[u] = unit < K::k_units ? page_of(t0 + unit / (D / 16)) : -1;
-            v_id[u] = unit < K::v_units ? page_of(t0 + unit / (D / 4) * 4) : -1;
+            k_id[u] = entry(t0 + k_token[u]);
+            v_id[u] = entry(t0 + v_token[u]);
         }
-        if (tid < K::groups) g_id = page_of(t0 + 16 * tid);
+        if (tid < K::groups) g_id = entry(t0 + 16 * tid);
     };
     const auto load = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int unit = tid + u * K::threads;
-            kw[u] = u32x4{0, 0, 0, 0};
-            if (k_id[u] >= 0) {
-                const int token = unit / (D / 16), c = unit % (D / 16);
-                kw[u] = *(const u32x4 *)(p.k + k_id[u] * p.k_page + h * p.k_head + ((t0 + token) & in_page) * D + 16 * c);
-            }
+            k_there[u] = valid(t0 + k_token[u], k_id[u]);
+            const int ki = k_there[u] ? k_id[u] : 0;
+            kw[u] = *(const u32x4 *)(p.k + ki * p.k_page + h * p.k_head + ((t0 + k_token[u]) & in_page) * D + k_at[u]);
+            v_there[u] = valid(t0 + v_token[u], v_id[u]);
+            const int vi = v_there[u] ? v_id[u] : 0;
+            const uint8_t *v = p.v + vi * p.v_page + h * p.v_head + ((t0 + v_token[u]) & in_page) * D + v_at[u];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) vw[u][r] = 0;
-            v_scale[u] = 1.f;
-            if (v_id[u] >= 0) {
-                const int token = unit / (D / 4) * 4, c = unit % (D / 4);
-                const uint8_t *v = p.v + v_id[u] * p.v_page + h * p.v_head + ((t0 + token) & in_page) * D + 4 * c;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vw[u][r] = *(const uint32_t *)(v + r * D);
-                if (!K::f16) v_scale[u] = p.v_scale[v_id[u] * p.vs_page + h];
-            }
+            for (int r = 0; r < 4; ++r) vw[u][r] = *(const uint32_t *)(v + r * D);
+            if (!K::f16) v_scale[u] = p.v_scale[vi * p.vs_page + h];
         }
         if (tid < K::groups) {
-            there = g_id >= 0;
-            ks = there ? p.k_scale[g_id * p.ks_page + h] : 0.f;
-            vs = there ? p.v_scale[g_id * p.vs_page + h] : 1.f;
+            there = valid(t0 + 16 * tid, g_id);
+            const int id = there ? g_id : 0;
+            ks = p.k_scale[id * p.ks_page + h];
+            vs = p.v_scale[id * p.vs_page + h];
         }
     };
     const auto store = [&](uint8_t *buf, int t0) __attribute__((always_inline)) {
         const bool hides = t0 + TN > plain;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int unit = tid + u * K::threads;
-            if (K::k_units % K::threads != 0 && unit >= K::k_units) continue;
+            if (K::k_units % K::threads != 0 && tid + u * K::threads >= K::k_units) continue;
             {
-                const int token = unit / (D / 16), c = unit % (D / 16);
                 u32x4 lo, hi;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    lo[2 * e] = Wide<T>::template two<false>(kw[u][e], 1.f);
-                    lo[2 * e + 1] = Wide<T>::template two<true>(kw[u][e], 1.f);
-                    hi[2 * e] = Wide<T>::template two<false>(kw[u][2 + e], 1.f);
-                    hi[2 * e + 1] = Wide<T>::template two<true>(kw[u][2 + e], 1.f);
+                    const uint32_t x = k_there[u] ? kw[u][e] : 0, y = k_there[u] ? kw[u][2 + e] : 0;
+                    lo[2 * e] = Wide<T>::template two<false>(x, 1.f);
+                    lo[2 * e + 1] = Wide<T>::template two<true>(x, 1.f);
+                    hi[2 * e] = Wide<T>::template two<false>(y, 1.f);
+                    hi[2 * e + 1] = Wide<T>::template two<true>(y, 1.f);
                 }
-                *(u32x4 *)(buf + token * K::k_pitch + 32 * c) = lo;
-                *(u32x4 *)(buf + token * K::k_pitch + 32 * c + 16) = hi;
+                *(u32x4 *)(buf + k_token[u] * K::k_pitch + 2 * k_at[u]) = lo;
+                *(u32x4 *)(buf + k_token[u] * K::k_pitch + 2 * k_at[u] + 16) = hi;
             }
-            const int token = unit / (D / 4) * 4, c = unit % (D / 4);
+            const int token = v_token[u], c = v_at[u] / 4;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vw[u][r] = v_there[u] ? vw[u][r] : 0;
             if (hides) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -219,13 +223,14 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // tokens 4t of 16 stand at 8 (t % 2) + 4 (t / 2), the order of S^T's result
             const int t = token >> 2, place = (token & ~15) + 8 * (t & 1) + 4 * ((t >> 1) & 1);
             uint8_t *const to = buf + K::k_bytes + 2 * place;
-            const float sv = K::f16 ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
+            const float sv = K::f16 || !v_there[u] ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
         }
         if (tid < K::groups) {
-            f32x4 x = {p.c * ks, there ? 0.f : -INFINITY, 1.f, 0.f};
+            f32x4 x = {there ? p.c * ks : 0.f, there ? 0.f : -INFINITY, 1.f, 0.f};
+            vs = there ? vs : 1.f;
             if (K::f16) {
                 const float v = fminf(fmaxf(vs, 0x1p-60f), 0x1p60f);
                 x[1] += __builtin_amdgcn_logf(v);
@@ -319,11 +324,11 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         look_up(from);
         load(from);
         look_up(from + TN);
-        __syncthreads(); // (first_nan)
+        lds_barrier(); // (first_nan)
         store(lds, from);
         load(from + TN);
         look_up(from + 2 * TN);
-        __syncthreads();
+        lds_barrier();
         int turn = 0;
         for (int t0 = from; t0 < end; t0 += TN) {
             if (t0 < wave_last) compute(lds + turn * K::buffer, t0);
@@ -333,10 +338,10 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
                 load(t0 + 2 * TN);
                 look_up(t0 + 3 * TN);
             }
-            __syncthreads();
+            lds_barrier();
         }
     } else {
-        __syncthreads();
+        lds_barrier();
     }
 
     // ---- the result ----

@@ -14,32 +14,34 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's chunks, for one row of a tile and head.  A block's lanes take
-// four elements of every (256 / (size / 4))-th chunk each; their sums are added in that order.
-template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size) {
-    const uint32_t row_of = blockIdx.x / (uint32_t)p.part_rows, number = row_of / (uint32_t)p.heads;
-    const int row = (int)(blockIdx.x - row_of * p.part_rows), h = (int)(row_of - number * p.heads);
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's chunks, for `at_once` rows of a tile and head.  A row's lanes take
+// four elements of every slices-th chunk each; their sums are added in that order.
+template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
+    const uint32_t parts = (uint32_t)(p.part_rows + at_once - 1) / at_once;
+    const uint32_t tile_of = blockIdx.x / parts, number = tile_of / (uint32_t)p.heads;
+    const int row0 = (int)(blockIdx.x - tile_of * parts) * at_once, h = (int)(tile_of - number * p.heads);
     const int chunk = chunk_of<R>(p);
     int b;
     uint32_t tile;
     if (!locate(number, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
     const Sequence s = sequence(p.seq, b);
-    const int chunks = (int)chunks_of(s, chunk);
-    if (chunks == 1 || s.rows * p.group - (int)tile * R <= row) return;
+    const int chunks = (int)chunks_of(s, chunk), rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
+    if (chunks == 1 || rows <= row0) return;
     uint32_t slot = 0; // slots before this sequence's
     for (int i = threadIdx.x & 63; i < b; i += 64) {
         const Sequence o = sequence(p.seq, i);
         slot += tiles_of<R>(p, o) * chunks_of(o, chunk);
     }
     slot = (uint32_t)wave_sum(slot) + tile * chunks;
+    const int quads = size / 4, slices = 256 / (quads * at_once);
+    const int unit = threadIdx.x / quads, slice = unit / at_once, row = row0 + unit - slice * at_once, d = 4 * (threadIdx.x - unit * quads);
+    const bool works = slice < slices && row < rows;
     const int64_t first = ((int64_t)slot * p.heads + h) * p.part_rows + row, step = (int64_t)p.heads * p.part_rows;
-    float m = -INFINITY;
-    for (int c = threadIdx.x & 63; c < chunks; c += 64) m = fmaxf(m, p.part_ml[2 * (first + c * step)]);
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    const int quads = size / 4, slices = 256 / quads, slice = threadIdx.x / quads, d = 4 * (threadIdx.x - slice * quads);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    if (slice < slices) {
+    float m = -INFINITY, l = 0.f;
+    if (works) {
+#pragma unroll 4
+        for (int c = 0; c < chunks; ++c) m = fmaxf(m, p.part_ml[2 * (first + c * step)]);
 #pragma unroll 4
         for (int c = slice; c < chunks; c += slices) {
             const int64_t i = first + c * step;
@@ -53,10 +55,10 @@ template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(
     part[threadIdx.x] = o;
     sum[threadIdx.x] = l;
     __syncthreads();
-    if (slice != 0) return;
+    if (slice != 0 || !works) return;
     for (int i = 1; i < slices; ++i) {
-        o += part[threadIdx.x + i * quads];
-        l += sum[threadIdx.x + i * quads];
+        o += part[threadIdx.x + i * at_once * quads];
+        l += sum[threadIdx.x + i * at_once * quads];
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     const int r = (int)tile * R + row, t = (int)quotient(r, p.group_magic, p.group_shift), head = r - t * p.group;
@@ -74,8 +76,9 @@ struct Plan {
     int64_t workspace;      // what a split call wants
 };
 
-// Blocks that a call is split up to: four of four waves on every compute unit.
-constexpr int64_t kBlocks = 4 * kComputeUnits;
+// Blocks that a call is split up to.  Few rows: four of four waves for every compute unit.  Many rows: as many as are resident, eight
+// waves a unit, all of one length.
+inline int64_t most_blocks(int tile_rows) { return kComputeUnits * (tile_rows <= 64 ? 4 : tile_rows == 128 ? 2 : 1); }
 
 int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     set_last_error("");
@@ -101,7 +104,7 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     const int64_t rows = (tokens * group + batch - 1) / batch;
     const int R = o->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && m.size <= 128 ? 64 : rows <= 128 ? 128 : 256;
     const int64_t tiles = tokens * group / R + (batch < tokens ? batch : tokens);
-    int64_t slots = kBlocks / m.heads;
+    int64_t slots = most_blocks(R) / m.heads;
     const bool split = may_split && slots > tiles;
     if (!split) slots = tiles;
     if (slots * m.heads >= 1ll << 23) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; } // (2^32 lanes)
@@ -132,12 +135,14 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
 int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream) {
     const auto run = [&](auto t) {
         typedef decltype(t) T;
-        const dim3 grid(tiles * p.heads * p.part_rows), block(256);
-        if (tile_rows == 16) hipLaunchKernelGGL((join_kernel<T, 16>), grid, block, 0, (hipStream_t)stream, p, size);
-        else if (tile_rows == 32) hipLaunchKernelGGL((join_kernel<T, 32>), grid, block, 0, (hipStream_t)stream, p, size);
-        else if (tile_rows == 64) hipLaunchKernelGGL((join_kernel<T, 64>), grid, block, 0, (hipStream_t)stream, p, size);
-        else if (tile_rows == 128) hipLaunchKernelGGL((join_kernel<T, 128>), grid, block, 0, (hipStream_t)stream, p, size);
-        else hipLaunchKernelGGL((join_kernel<T, 256>), grid, block, 0, (hipStream_t)stream, p, size);
+        // few rows have many chunks: a row a block; many rows as many as its lanes hold
+        const int at_once = tile_rows <= 64 ? 1 : 256 / (size / 4);
+        const dim3 grid(tiles * p.heads * ((p.part_rows + at_once - 1) / at_once)), block(256);
+        if (tile_rows == 16) hipLaunchKernelGGL((join_kernel<T, 16>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
+        else if (tile_rows == 32) hipLaunchKernelGGL((join_kernel<T, 32>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
+        else if (tile_rows == 64) hipLaunchKernelGGL((join_kernel<T, 64>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
+        else if (tile_rows == 128) hipLaunchKernelGGL((join_kernel<T, 128>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
+        else hipLaunchKernelGGL((join_kernel<T, 256>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
     };
     if (dtype == MCF_F16) run((_Float16)0);
     else run((__bf16)0);
