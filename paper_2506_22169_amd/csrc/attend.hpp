@@ -4,17 +4,27 @@
 // query head r % group of token r / group.  Rows go to blocks in tiles of R; the tokens that a tile sees are split into
 // chunks where tiles are few.  A slot is one chunk of one tile, a block one slot of one head.
 //
-// How long sequences are only the device knows, so the blocks find their slot themselves: the host gives a number of slots
-// S that leaves room for chunks beside the tiles, and with T tiles and W = sum of tiles times tokens
+// How long sequences are only the device knows, so the blocks find their work themselves; the host gives numbers of blocks.
+//
+// Few rows (attend_rows.hpp).  All tiles' tokens, in units of kUnit and one unit more for each tile (what it costs beside its
+// tokens), form one line, that the blocks of a head cut into equal pieces: a block goes through the tiles that its piece touches.  A
+// tile that lies in one piece is written by its block; of the others the block leaves a part in the workspace (at most two a block:
+// its first tile and its last), and a second kernel joins the parts of each tile that a cut goes through.
+//
+// Many rows (attend_tiles.hpp).  A block takes one chunk of one tile.  With S slots for a head, T tiles and W = sum of tiles
+// times tokens
 //     chunk = W / (S - T), rounded up      =>      sum over tiles of ceil(tokens / chunk) <= W / chunk + T <= S.
-// Sequences of any mix of lengths are cut into equal pieces that way, and a block holds one piece of one tile only.
 #pragma once
 #include "sequences.hpp"
 
 namespace mcf {
 namespace attend {
 
-constexpr int kStep = 128;     // chunks are multiples of this many tokens
+constexpr int kUnit = 128; // tokens that pieces and chunks are multiples of
+constexpr int kLeast = 2;  // units of a piece, at least
+
+// attend_rows.hpp: waves that a SIMD's registers hold (left to itself the compiler spends them on fewer, and the loads in flight are what the kernel waits for).
+constexpr int waves_per_simd(int D, int NB) { return NB == 1 ? (D <= 64 ? 4 : D <= 128 ? 3 : 2) : NB == 2 ? (D <= 64 ? 3 : D <= 128 ? 2 : 1) : D <= 64 ? 2 : 1; }
 
 struct Params {
     Sequences seq;
@@ -31,7 +41,7 @@ struct Params {
     int32_t causal, split;
     int32_t pages, heads, group, page_log;
     int32_t part_rows;
-    uint32_t slots;
+    uint32_t slots; // blocks of a head (few rows, split: pieces)
     uint32_t group_magic;
     int32_t group_shift;
 };
@@ -48,7 +58,35 @@ template <int R> __device__ __forceinline__ uint32_t tiles_of(const Params &p, c
     return (uint32_t)(((int64_t)s.rows * p.group + R - 1) / R);
 }
 
-// Tokens of a chunk.
+// ---- few rows: pieces of the line ----
+__device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
+// Units of a piece; *total: of the line (the host has seen to it that it fits)
+template <int R> __device__ __forceinline__ uint32_t piece_of(const Params &p, uint32_t *total) {
+    uint32_t n = 0;
+    for (int b = threadIdx.x & 63; b < p.seq.batch; b += 64) {
+        const Sequence s = sequence(p.seq, b);
+        n += tiles_of<R>(p, s) * units_of(s);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+    *total = __builtin_amdgcn_readfirstlane(n);
+    const uint32_t piece = (*total + p.slots - 1) / p.slots;
+    return piece < kLeast ? kLeast : piece;
+}
+// Place in the line: the sequence and the units before it there.
+template <int R> __device__ __forceinline__ bool locate_unit(const Params &p, uint32_t at, int *b, uint32_t *rest) {
+    const bool found = locate(at, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
+        const Sequence s = sequence(p.seq, i);
+        return tiles_of<R>(p, s) * units_of(s);
+    }, b, rest);
+    *b = __builtin_amdgcn_readfirstlane(*b);
+    *rest = __builtin_amdgcn_readfirstlane(*rest);
+    return found;
+}
+// The token at which unit x of a tile begins (the first unit has none).
+__device__ __forceinline__ int first_token(uint32_t x) { return x > 0 ? (int)(x - 1) * kUnit : 0; }
+
+// ---- many rows: chunks ----
 template <int R> __device__ __forceinline__ int chunk_of(const Params &p) {
     if (!p.split) return 0x7fffff80;
     const int lane = threadIdx.x & 63;
@@ -63,8 +101,8 @@ template <int R> __device__ __forceinline__ int chunk_of(const Params &p) {
     tiles = wave_sum(tiles);
     const int64_t room = (int64_t)p.slots - tiles;
     if (room <= 0) return 0x7fffff80;
-    const int64_t chunk = ((work + room - 1) / room + kStep - 1) / kStep * kStep;
-    return chunk < kStep ? kStep : chunk < 0x7fffff80 ? (int)chunk : 0x7fffff80;
+    const int64_t chunk = ((work + room - 1) / room + kUnit - 1) / kUnit * kUnit;
+    return chunk < kUnit ? kUnit : chunk < 0x7fffff80 ? (int)chunk : 0x7fffff80;
 }
 __device__ __forceinline__ uint32_t chunks_of(const Sequence &s, int chunk) { return s.seen > chunk ? (uint32_t)((s.seen - 1) / chunk) + 1 : 1u; }
 
@@ -78,7 +116,6 @@ int launch_rows_f16(const Params &p, int size, int row_blocks, unsigned blocks, 
 int launch_rows_bf16(const Params &p, int size, int row_blocks, unsigned blocks, void *stream);
 int launch_tiles_f16(const Params &p, int size, int waves, unsigned blocks, void *stream);
 int launch_tiles_bf16(const Params &p, int size, int waves, unsigned blocks, void *stream);
-int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream);
 
 } // namespace attend
 } // namespace mcf

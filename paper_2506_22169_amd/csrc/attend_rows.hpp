@@ -91,14 +91,17 @@ template <typename T, int D, int NB> struct Rows {
     // element of the contraction that lane group g holds first in step s (8 of them; both operands alike)
     static __device__ __forceinline__ int part(int s, int g) { return Step<D>::wide ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g; }
 
-    static __device__ __forceinline__ void load(const Params &p, int b, int h, int t, int end, Step<D> &x) {
+    // The table's entries for the 32 tokens from t, as they stand there: asked for a step before they are looked at.
+    static __device__ __forceinline__ void look_up(const Params &p, const int32_t *table, int t, int seen, int id[2]) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) id[j] = table[(t + 16 * j < seen ? t + 16 * j : seen - 1) >> p.page_log];
+    }
+    static __device__ __forceinline__ void load(const Params &p, int h, int t, int seen, const int ids[2], Step<D> &x) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int at = t + 16 * j;
-            int id = at < end ? p.seq.table[b * p.seq.table_stride + (at >> p.page_log)] : -1;
-            id = __builtin_amdgcn_readfirstlane(id);
-            const bool there = id >= 0 && id < p.pages;
+            const int at = t + 16 * j, id = __builtin_amdgcn_readfirstlane(ids[j]);
+            const bool there = at < seen && id >= 0 && id < p.pages;
             x.hide[j] = there ? 0.f : -INFINITY;
             if (!there) {
                 x.sk[j] = 0.f;
@@ -272,29 +275,18 @@ template <typename T, int D, int NB> struct Rows {
     }
 };
 
-template <typename T, int D, int NB> __global__ __launch_bounds__(256) void rows_kernel(const Params p) {
+// The rows of one tile over its tokens from .. to - 1 (as far as it sees any); part < 0: all of them, the result is written; else what
+// they give goes to that place of the workspace.
+template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(const Params &p, int b, int h, uint32_t tile, int from, int to, int part_at) {
     typedef Rows<T, D, NB> K;
     typedef Cols<D> C;
     constexpr int R = K::R, pitch = D + 4;
-    const uint32_t slot = blockIdx.x / (uint32_t)p.heads;
-    const int h = (int)(blockIdx.x - slot * p.heads);
-    const int chunk = __builtin_amdgcn_readfirstlane(chunk_of<R>(p));
-    int b;
-    uint32_t rest;
-    if (!locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
-            const Sequence s = sequence(p.seq, i);
-            return tiles_of<R>(p, s) * chunks_of(s, chunk);
-        }, &b, &rest)) return;
-    b = __builtin_amdgcn_readfirstlane(b);
-    rest = __builtin_amdgcn_readfirstlane(rest);
     const Sequence s = sequence(p.seq, b);
-    const uint32_t chunks = chunks_of(s, chunk), tile = rest / chunks, ch = rest - tile * chunks;
     const int rows = s.rows * p.group - (int)tile * R; // of this tile, of R
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const auto token_of = [&](int r) __attribute__((always_inline)) { return (int)quotient(tile * R + r, p.group_magic, p.group_shift); };
     const int last = limit_of(p, s, token_of(rows < R ? rows - 1 : R - 1)), all = limit_of(p, s, token_of(0));
-    const int64_t from = (int64_t)ch * chunk;
-    const int end = from + chunk < last ? (int)from + chunk : last; // the tile's tokens in this chunk: from .. end - 1
+    const int end = to < last ? to : last;
 
     typename K::State st;
 #pragma unroll
@@ -315,24 +307,32 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) void rows
 #pragma unroll
         for (int c = 0; c < C::tiles; ++c) st.o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    int t = (int)(from < end ? from : end) + 32 * wave;
+    const int32_t *const table = p.seq.table + b * p.seq.table_stride;
+    int t = (from < end ? from : end) + 32 * wave;
     const int plain = all < end ? all : end; // every row sees the tokens below
+    int id[2];
+    if (t < end) K::look_up(p, table, t, s.seen, id);
     if (t + 32 <= plain) {
         Step<D> x, next;
-        K::load(p, b, h, t, s.seen, x);
+        K::load(p, h, t, s.seen, id, x);
+        K::look_up(p, table, t + kUnit, s.seen, id);
         for (;;) {
-            const int u = t + kStep;
+            const int u = t + kUnit;
             const bool more = u + 32 <= plain;
-            if (more) K::load(p, b, h, u, s.seen, next);
+            if (more) {
+                K::load(p, h, u, s.seen, id, next);
+                K::look_up(p, table, u + kUnit, s.seen, id);
+            }
             K::template step<false>(p, x, t, end, all, st);
             t = u;
             if (!more) break;
             x = next;
         }
     }
-    for (; t < end; t += kStep) {
+    for (; t < end; t += kUnit) {
         Step<D> x;
-        K::load(p, b, h, t, s.seen, x);
+        K::load(p, h, t, s.seen, id, x);
+        K::look_up(p, table, t + kUnit, s.seen, id);
         K::template step<true>(p, x, t, end, all, st);
     }
 
@@ -345,7 +345,7 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) void rows
         st.l[n] += __shfl_xor(st.l[n], 32);
         if (g == 0) { ref[wave][16 * n + i] = st.m[n]; sum[wave][16 * n + i] = st.l[n]; }
     }
-    const int64_t place = ((int64_t)slot * p.heads + h) * p.part_rows;
+    const int64_t place = ((int64_t)part_at * p.heads + h) * p.part_rows;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         __syncthreads();
@@ -367,7 +367,7 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) void rows
             float l = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) l += ref[w][row] == -INFINITY ? sum[w][row] : sum[w][row] * __builtin_amdgcn_exp2f(ref[w][row] - top); // (nothing seen: 0, or NaN by NaN scores)
-            if (chunks > 1) {
+            if (part_at >= 0) {
                 *(f32x4 *)(p.part + (place + row) * D + d) = o;
                 if (d == 0) { p.part_ml[2 * (place + row)] = top; p.part_ml[2 * (place + row) + 1] = l; }
             } else {
@@ -380,6 +380,41 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) void rows
                 *(T4 *)((T *)p.out + (int64_t)(s.first + tk) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
             }
         }
+    }
+    __syncthreads(); // (the shared parts are free again)
+}
+
+template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_simd(D, NB), waves_per_simd(D, NB)))) void rows_kernel(const Params p) {
+    typedef Rows<T, D, NB> K;
+    constexpr int R = K::R;
+    const uint32_t j = blockIdx.x / (uint32_t)p.heads;
+    const int h = (int)(blockIdx.x - j * p.heads);
+    int b;
+    uint32_t rest, at = 0, end = 1;
+    if (p.split) {
+        uint32_t total;
+        const uint32_t piece = piece_of<R>(p, &total);
+        at = j * piece;
+        end = at + piece < total ? at + piece : total;
+        if (at >= end || !locate_unit<R>(p, at, &b, &rest)) return;
+    } else { // tile j, as the one unit of a piece
+        if (!locate(j, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &rest)) return;
+        b = __builtin_amdgcn_readfirstlane(b);
+        rest = __builtin_amdgcn_readfirstlane(rest);
+    }
+    for (;;) {
+        const Sequence s = sequence(p.seq, b);
+        const uint32_t units = p.split ? units_of(s) : 1, all = units * tiles_of<R>(p, s);
+        while (rest < all && at < end) {
+            const uint32_t tile = rest / units, x = rest - tile * units, n = units - x < end - at ? units - x : end - at;
+            const int from = first_token(x), to = x + n == units ? 0x7fffffff : first_token(x + n);
+            if (from < to) tile_part<T, D, NB>(p, b, h, tile, from, to, from == 0 && x + n == units ? -1 : (int)(2 * j + (from == 0)));
+            rest += n;
+            at += n;
+        }
+        if (at >= end) return;
+        rest = 0;
+        if (++b >= p.seq.batch) return;
     }
 }
 

@@ -14,40 +14,32 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's chunks, for `at_once` rows of a tile and head.  A row's lanes take
-// four elements of every slices-th chunk each; their sums are added in that order.
-template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
-    const uint32_t parts = (uint32_t)(p.part_rows + at_once - 1) / at_once;
-    const uint32_t tile_of = blockIdx.x / parts, number = tile_of / (uint32_t)p.heads;
-    const int row0 = (int)(blockIdx.x - tile_of * parts) * at_once, h = (int)(tile_of - number * p.heads);
-    const int chunk = chunk_of<R>(p);
-    int b;
-    uint32_t tile;
-    if (!locate(number, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
-    const Sequence s = sequence(p.seq, b);
-    const int chunks = (int)chunks_of(s, chunk), rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
-    if (chunks == 1 || rows <= row0) return;
-    uint32_t slot = 0; // slots before this sequence's
-    for (int i = threadIdx.x & 63; i < b; i += 64) {
-        const Sequence o = sequence(p.seq, i);
-        slot += tiles_of<R>(p, o) * chunks_of(o, chunk);
-    }
-    slot = (uint32_t)wave_sum(slot) + tile * chunks;
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's parts, for `at_once` rows of a tile and head; part i stands at
+// place(i) of the workspace.  A row's lanes take four elements of every slices-th part each; their sums are added in that order.
+template <typename T, int R, typename F>
+__device__ __forceinline__ void join(const Params &p, const Sequence &s, int h, uint32_t tile, int row0, int at_once, int size, int parts, F place) {
+    const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
+    if (rows <= row0) return;
     const int quads = size / 4, slices = 256 / (quads * at_once);
-    const int unit = threadIdx.x / quads, slice = unit / at_once, row = row0 + unit - slice * at_once, d = 4 * (threadIdx.x - unit * quads);
+    const int unit = threadIdx.x / quads, slice = unit / at_once, row = at_once == 1 ? row0 : row0 + unit - slice * at_once, d = 4 * (threadIdx.x - unit * quads);
     const bool works = slice < slices && row < rows;
-    const int64_t first = ((int64_t)slot * p.heads + h) * p.part_rows + row, step = (int64_t)p.heads * p.part_rows;
+    const auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)place(i) * p.heads + h) * p.part_rows + row; };
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
+    if (at_once == 1) { // one row for the whole wave
+        for (int i = threadIdx.x & 63; i < parts; i += 64) m = fmaxf(m, p.part_ml[2 * at(i)]);
+        for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+    } else if (works) {
+#pragma unroll 4
+        for (int i = 0; i < parts; ++i) m = fmaxf(m, p.part_ml[2 * at(i)]);
+    }
     if (works) {
 #pragma unroll 4
-        for (int c = 0; c < chunks; ++c) m = fmaxf(m, p.part_ml[2 * (first + c * step)]);
-#pragma unroll 4
-        for (int c = slice; c < chunks; c += slices) {
-            const int64_t i = first + c * step;
-            const float mi = p.part_ml[2 * i], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m); // (nothing seen: zeros, or NaN)
-            l += p.part_ml[2 * i + 1] * by;
-            o += *(const f32x4 *)(p.part + i * size + d) * by;
+        for (int i = slice; i < parts; i += slices) {
+            const int64_t a = at(i);
+            const float mi = p.part_ml[2 * a], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m); // (nothing seen: zeros, or NaN)
+            l += p.part_ml[2 * a + 1] * by;
+            o += *(const f32x4 *)(p.part + a * size + d) * by;
         }
     }
     __shared__ f32x4 part[256];
@@ -69,16 +61,77 @@ template <typename T, int R> __global__ __launch_bounds__(256) void join_kernel(
     *(T4 *)((T *)p.out + (int64_t)(s.first + t) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
 }
 
+// Many rows: a block looks after at_once rows of a tile, whatever its chunks.
+template <typename T, int R> __global__ __launch_bounds__(256) void join_chunks_kernel(const Params p, int size, int at_once) {
+    const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once;
+    const uint32_t tile_of = blockIdx.x / groups, number = tile_of / (uint32_t)p.heads;
+    const int row0 = (int)(blockIdx.x - tile_of * groups) * at_once, h = (int)(tile_of - number * p.heads);
+    const int chunk = chunk_of<R>(p);
+    int b;
+    uint32_t tile;
+    if (!locate(number, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
+    const Sequence s = sequence(p.seq, b);
+    const int chunks = (int)chunks_of(s, chunk);
+    if (chunks == 1) return;
+    uint32_t slot = 0; // slots before this sequence's
+    for (int i = threadIdx.x & 63; i < b; i += 64) {
+        const Sequence o = sequence(p.seq, i);
+        slot += tiles_of<R>(p, o) * chunks_of(o, chunk);
+    }
+    slot = (uint32_t)wave_sum(slot) + tile * chunks;
+    join<T, R>(p, s, h, tile, row0, at_once, size, chunks, [&](int i) __attribute__((always_inline)) { return slot + i; });
+}
+
+// Few rows: a block looks after at_once rows of a tile.  BY_TILE: tile number j; else the tile that cut j + 1 (between pieces j
+// and j + 1) goes through, if no cut before it does: whichever are fewer.
+template <typename T, int R, bool BY_TILE> __global__ __launch_bounds__(256) void join_pieces_kernel(const Params p, int size, int at_once) {
+    const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once;
+    const uint32_t number = blockIdx.x / groups;
+    uint32_t j = number / (uint32_t)p.heads, total, rest, tile, x;
+    const int row0 = (int)(blockIdx.x - number * groups) * at_once, h = (int)(number - j * p.heads);
+    const uint32_t piece = piece_of<R>(p, &total);
+    int b;
+    if (BY_TILE) {
+        if (!locate(j, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
+    } else {
+        if (++j * piece >= total || !locate_unit<R>(p, j * piece, &b, &rest)) return;
+    }
+    const Sequence s = sequence(p.seq, b);
+    const uint32_t units = units_of(s);
+    if (BY_TILE) { // its first cut behind a token
+        uint32_t before = 0;
+        for (int i = threadIdx.x & 63; i < b; i += 64) {
+            const Sequence o = sequence(p.seq, i);
+            before += tiles_of<R>(p, o) * units_of(o);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
+        before += tile * units;
+        j = (before + 1) / piece + 1;
+        x = j * piece - before;
+        if (x >= units) return;
+    } else {
+        tile = rest / units;
+        x = rest - tile * units;
+        if (x < 2 || x >= piece + 2) return; // no token before the cut; another cut before it
+    }
+    const int parts = 1 + (int)((units - x + piece - 1) / piece);
+    join<T, R>(p, s, h, tile, row0, at_once, size, parts, [&](int i) __attribute__((always_inline)) { return i ? 2 * (j + i - 1) : 2 * j - 1; });
+}
+
 struct Plan {
     Params p;
     int tile_rows;          // 16, 32, 64: attend_rows.hpp; 128, 256: attend_tiles.hpp
     unsigned tiles, blocks; // an upper bound of the tiles; 0 blocks: nothing to do
     int64_t workspace;      // what a split call wants
+    int64_t places;         // of parts there
 };
 
-// Blocks that a call is split up to.  Few rows: four of four waves for every compute unit.  Many rows: as many as are resident, eight
-// waves a unit, all of one length.
-inline int64_t most_blocks(int tile_rows) { return kComputeUnits * (tile_rows <= 64 ? 4 : tile_rows == 128 ? 2 : 1); }
+// Blocks that are resident at once, by the registers (attend_rows.hpp: waves_per_simd; attend_tiles.hpp: two waves a SIMD).
+inline int64_t resident_blocks(int tile_rows, int64_t size) {
+    if (tile_rows > 64) return kComputeUnits * (tile_rows == 128 ? 2 : 1);
+    return kComputeUnits * waves_per_simd((int)size, tile_rows / 16);
+}
 
 int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     set_last_error("");
@@ -104,9 +157,20 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     const int64_t rows = (tokens * group + batch - 1) / batch;
     const int R = o->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && m.size <= 128 ? 64 : rows <= 128 ? 128 : 256;
     const int64_t tiles = tokens * group / R + (batch < tokens ? batch : tokens);
-    int64_t slots = most_blocks(R) / m.heads;
-    const bool split = may_split && slots > tiles;
-    if (!split) slots = tiles;
+    int64_t slots = resident_blocks(R, m.size) / m.heads;
+    bool split = may_split;
+    if (R > 64) {
+        split = split && slots > tiles;
+        if (!split) slots = tiles;
+    } else {
+        // no more pieces than the longest sequences that the table holds would give; the line in 31 bits
+        const int64_t most = tiles * ((m.pages ? c->seq.table_width * m.page_size : 0) / kUnit + 2);
+        if (slots < 1) slots = 1;
+        if (slots > (most + kLeast - 1) / kLeast) slots = (most + kLeast - 1) / kLeast;
+        split = split && most < 1ll << 31;
+        if (!split) slots = tiles;
+    }
+    const int64_t places = R > 64 ? slots : 2 * slots; // of parts in the workspace
     if (slots * m.heads >= 1ll << 23) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; } // (2^32 lanes)
     Params &p = o->p;
     p.seq = device_sequences(c->seq, m.page_size);
@@ -126,23 +190,28 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     division_magic((uint32_t)group, &p.group_magic, &p.group_shift);
     o->tiles = (unsigned)tiles;
     o->blocks = (unsigned)(slots * m.heads);
-    if (split) o->workspace = slots * m.heads * p.part_rows * (m.size + 2) * 4;
+    o->places = places * m.heads;
+    if (split) o->workspace = o->places * p.part_rows * (m.size + 2) * 4;
     return MCF_OK;
 }
 
 } // namespace
 
-int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream) {
+static int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream) {
     const auto run = [&](auto t) {
         typedef decltype(t) T;
-        // few rows have many chunks: a row a block; many rows as many as its lanes hold
-        const int at_once = tile_rows <= 64 ? 1 : 256 / (size / 4);
-        const dim3 grid(tiles * p.heads * ((p.part_rows + at_once - 1) / at_once)), block(256);
-        if (tile_rows == 16) hipLaunchKernelGGL((join_kernel<T, 16>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
-        else if (tile_rows == 32) hipLaunchKernelGGL((join_kernel<T, 32>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
-        else if (tile_rows == 64) hipLaunchKernelGGL((join_kernel<T, 64>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
-        else if (tile_rows == 128) hipLaunchKernelGGL((join_kernel<T, 128>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
-        else hipLaunchKernelGGL((join_kernel<T, 256>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
+        // a row a block where a tile has many parts (all lanes share them out), else as many rows as the lanes hold
+        const int at_once = tile_rows <= 64 && p.slots >= 8 * tiles ? 1 : 256 / (size / 4);
+        const unsigned groups = (unsigned)(p.part_rows + at_once - 1) / at_once;
+        const bool by_tile = tiles < p.slots;
+        const dim3 chunks(tiles * p.heads * groups), pieces((by_tile ? tiles : p.slots - 1) * p.heads * groups), block(256);
+        hipStream_t st = (hipStream_t)stream;
+        if (tile_rows == 128) hipLaunchKernelGGL((join_chunks_kernel<T, 128>), chunks, block, 0, st, p, size, at_once);
+        else if (tile_rows == 256) hipLaunchKernelGGL((join_chunks_kernel<T, 256>), chunks, block, 0, st, p, size, at_once);
+        else if (p.slots == 1) return;
+        else if (tile_rows == 16) by_tile ? join_pieces_kernel<T, 16, true><<<pieces, block, 0, st>>>(p, size, at_once) : join_pieces_kernel<T, 16, false><<<pieces, block, 0, st>>>(p, size, at_once);
+        else if (tile_rows == 32) by_tile ? join_pieces_kernel<T, 32, true><<<pieces, block, 0, st>>>(p, size, at_once) : join_pieces_kernel<T, 32, false><<<pieces, block, 0, st>>>(p, size, at_once);
+        else by_tile ? join_pieces_kernel<T, 64, true><<<pieces, block, 0, st>>>(p, size, at_once) : join_pieces_kernel<T, 64, false><<<pieces, block, 0, st>>>(p, size, at_once);
     };
     if (dtype == MCF_F16) run((_Float16)0);
     else run((__bf16)0);
@@ -180,7 +249,7 @@ extern "C" int mcf_cache_attention(const mcf_attention_call *c, void *workspace,
     attend::Params &p = l.p;
     if (l.workspace > 0) {
         p.part = (float *)workspace;
-        p.part_ml = p.part + (int64_t)l.blocks * p.part_rows * c->cache.size;
+        p.part_ml = p.part + l.places * p.part_rows * c->cache.size;
     }
     const int size = (int)c->cache.size;
     const bool f16 = c->dtype == MCF_F16;
