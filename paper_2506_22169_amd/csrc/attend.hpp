@@ -9,11 +9,14 @@
 // Few rows (attend_rows.hpp).  All tiles' tokens, in units of kUnit and one unit more for each tile (what it costs beside its
 // tokens), form one line, that the blocks of a head cut into equal pieces: a block goes through the tiles that its piece touches.  A
 // tile that lies in one piece is written by its block; of the others the block leaves a part in the workspace (at most two a block:
-// its first tile and its last), and a second kernel joins the parts of each tile that a cut goes through.
+// its first tile and its last).
 //
 // Many rows (attend_tiles.hpp).  A block takes one chunk of one tile.  With S slots for a head, T tiles and W = sum of tiles
 // times tokens
 //     chunk = W / (S - T), rounded up      =>      sum over tiles of ceil(tokens / chunk) <= W / chunk + T <= S.
+//
+// The block that leaves a tile's first part also notes where the others will stand (Split), and a second kernel, a block for each
+// that there was, joins them.
 #pragma once
 #include "sequences.hpp"
 
@@ -26,6 +29,11 @@ constexpr int kLeast = 2;  // units of a piece, at least
 // attend_rows.hpp: waves that a SIMD's registers hold (left to itself the compiler spends them on fewer, and the loads in flight are what the kernel waits for).
 constexpr int waves_per_simd(int D, int NB) { return NB == 1 ? (D <= 64 ? 4 : D <= 128 ? 3 : 2) : NB == 2 ? (D <= 64 ? 3 : D <= 128 ? 2 : 1) : D <= 64 ? 2 : 1; }
 
+// A tile in parts: how many (0: none), where the first and the second stand and the step from there; its first row and the rows.
+struct Split {
+    int32_t parts, first, second, step, token, row, rows, pad;
+};
+
 struct Params {
     Sequences seq;
     const void *q;
@@ -35,8 +43,9 @@ struct Params {
     const float *k_scale, *v_scale;
     int64_t k_page, k_head, v_page, v_head;
     int64_t ks_page, vs_page;
-    float *part;     // [slots * heads][part_rows][size]: what a chunk leaves
-    float *part_ml;  // [slots * heads][part_rows][2]: its reference exponent and its sum
+    float *part;     // [places * heads][part_rows][size]: what a part leaves
+    float *part_ml;  // [places * heads][part_rows][2]: its reference exponent and its sum
+    Split *splits;   // [slots * heads]: the tile whose first part the block wrote
     float c;         // scale * log2(e)
     int32_t causal, split;
     int32_t pages, heads, group, page_log;
@@ -60,28 +69,45 @@ template <int R> __device__ __forceinline__ uint32_t tiles_of(const Params &p, c
 
 // ---- few rows: pieces of the line ----
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
-// Units of a piece; *total: of the line (the host has seen to it that it fits)
-template <int R> __device__ __forceinline__ uint32_t piece_of(const Params &p, uint32_t *total) {
-    uint32_t n = 0;
-    for (int b = threadIdx.x & 63; b < p.seq.batch; b += 64) {
-        const Sequence s = sequence(p.seq, b);
-        n += tiles_of<R>(p, s) * units_of(s);
+// Piece j of the line: its first unit and the one behind it, and where the first lies: the sequence and the units before it there.
+// False: beyond the line.  Up to 64 sequences are read once, a lane each (two passes over more of them).
+template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uint32_t j, uint32_t *piece, uint32_t *at, uint32_t *end, int *b, uint32_t *rest, Sequence *s) {
+    const int lane = threadIdx.x & 63;
+    const auto units = [&](const Sequence &q) __attribute__((always_inline)) { return tiles_of<R>(p, q) * units_of(q); };
+    const auto cut = [&](uint32_t total) __attribute__((always_inline)) {
+        const uint32_t n = (total + p.slots - 1) / p.slots;
+        *piece = n < kLeast ? kLeast : n;
+        *at = j * *piece;
+        *end = *at + *piece < total ? *at + *piece : total;
+        return *at < total;
+    };
+    if (p.seq.batch <= 64) {
+        Sequence q = {0, 0, 0, 0};
+        if (lane < p.seq.batch) q = sequence(p.seq, lane);
+        const uint32_t n = units(q);
+        uint32_t upto = n;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t x = __shfl_up(upto, d);
+            if (lane >= d) upto += x;
+        }
+        if (!cut(__builtin_amdgcn_readlane(upto, 63))) return false;
+        const int i = __builtin_ctzll(__ballot(*at - (upto - n) < n));
+        *b = i;
+        *rest = *at - (__builtin_amdgcn_readlane(upto, i) - __builtin_amdgcn_readlane(n, i));
+        *s = {__builtin_amdgcn_readlane(q.first, i), __builtin_amdgcn_readlane(q.rows, i), __builtin_amdgcn_readlane(q.length, i), __builtin_amdgcn_readlane(q.seen, i)};
+        return true;
     }
+    uint32_t n = 0;
+    for (int i = lane; i < p.seq.batch; i += 64) n += units(sequence(p.seq, i));
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
-    *total = __builtin_amdgcn_readfirstlane(n);
-    const uint32_t piece = (*total + p.slots - 1) / p.slots;
-    return piece < kLeast ? kLeast : piece;
-}
-// Place in the line: the sequence and the units before it there.
-template <int R> __device__ __forceinline__ bool locate_unit(const Params &p, uint32_t at, int *b, uint32_t *rest) {
-    const bool found = locate(at, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
-        const Sequence s = sequence(p.seq, i);
-        return tiles_of<R>(p, s) * units_of(s);
-    }, b, rest);
+    if (!cut(__builtin_amdgcn_readfirstlane(n)) || !locate(*at, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return units(sequence(p.seq, i)); }, b, rest))
+        return false;
     *b = __builtin_amdgcn_readfirstlane(*b);
     *rest = __builtin_amdgcn_readfirstlane(*rest);
-    return found;
+    *s = sequence(p.seq, *b);
+    return true;
 }
 // The token at which unit x of a tile begins (the first unit has none).
 __device__ __forceinline__ int first_token(uint32_t x) { return x > 0 ? (int)(x - 1) * kUnit : 0; }

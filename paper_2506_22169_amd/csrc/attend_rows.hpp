@@ -277,11 +277,10 @@ template <typename T, int D, int NB> struct Rows {
 
 // The rows of one tile over its tokens from .. to - 1 (as far as it sees any); part < 0: all of them, the result is written; else what
 // they give goes to that place of the workspace.
-template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(const Params &p, int b, int h, uint32_t tile, int from, int to, int part_at) {
+template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(const Params &p, const Sequence &s, int b, int h, uint32_t tile, int from, int to, int part_at) {
     typedef Rows<T, D, NB> K;
     typedef Cols<D> C;
     constexpr int R = K::R, pitch = D + 4;
-    const Sequence s = sequence(p.seq, b);
     const int rows = s.rows * p.group - (int)tile * R; // of this tile, of R
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const auto token_of = [&](int r) __attribute__((always_inline)) { return (int)quotient(tile * R + r, p.group_magic, p.group_shift); };
@@ -390,32 +389,37 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribu
     const uint32_t j = blockIdx.x / (uint32_t)p.heads;
     const int h = (int)(blockIdx.x - j * p.heads);
     int b;
-    uint32_t rest, at = 0, end = 1;
+    uint32_t rest, at = 0, end = 1, piece = 1;
+    Sequence s;
+    Split split = {0, 0, 0, 0, 0, 0, 0, 0};
     if (p.split) {
-        uint32_t total;
-        const uint32_t piece = piece_of<R>(p, &total);
-        at = j * piece;
-        end = at + piece < total ? at + piece : total;
-        if (at >= end || !locate_unit<R>(p, at, &b, &rest)) return;
+        if (!find_piece<R>(p, j, &piece, &at, &end, &b, &rest, &s)) at = end = 0;
     } else { // tile j, as the one unit of a piece
         if (!locate(j, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &rest)) return;
         b = __builtin_amdgcn_readfirstlane(b);
         rest = __builtin_amdgcn_readfirstlane(rest);
+        s = sequence(p.seq, b);
     }
-    for (;;) {
-        const Sequence s = sequence(p.seq, b);
+    while (at < end) {
         const uint32_t units = p.split ? units_of(s) : 1, all = units * tiles_of<R>(p, s);
         while (rest < all && at < end) {
             const uint32_t tile = rest / units, x = rest - tile * units, n = units - x < end - at ? units - x : end - at;
             const int from = first_token(x), to = x + n == units ? 0x7fffffff : first_token(x + n);
-            if (from < to) tile_part<T, D, NB>(p, b, h, tile, from, to, from == 0 && x + n == units ? -1 : (int)(2 * j + (from == 0)));
+            const bool whole = from == 0 && x + n == units;
+            if (from < to) tile_part<T, D, NB>(p, s, b, h, tile, from, to, whole ? -1 : (int)(2 * j + (from == 0)));
+            if (from == 0 && to > 0 && !whole) { // the first of several parts
+                const int rows = s.rows * p.group - (int)tile * R;
+                split = {1 + (int)((units - x - n + piece - 1) / piece), (int)(2 * j + 1), (int)(2 * j + 2), 2, s.first, (int)tile * R, rows < R ? rows : R, 0};
+            }
             rest += n;
             at += n;
         }
-        if (at >= end) return;
+        if (at >= end) break;
         rest = 0;
-        if (++b >= p.seq.batch) return;
+        if (++b >= p.seq.batch) break;
+        s = sequence(p.seq, b);
     }
+    if (p.split && threadIdx.x == 0) p.splits[blockIdx.x] = split;
 }
 
 template <typename T> int launch_rows(const Params &p, int size, int row_blocks, unsigned blocks, void *stream) {

@@ -13,8 +13,8 @@
 //    neighbouring columns of the result.
 //  - Padding of 16 bytes a row puts the rows of both on different banks.
 //
-// Weights and what rows do not see: as in attend_rows.hpp, but with the power of two of V's scale in V for bf16 (what the scale is beyond
-// that, in the weights before they are rounded).  A NaN in V that only some
+// Weights and what rows do not see: as attend_rows.hpp does it for fp16, but for bf16 the power of two of V's scale is in V and only what it is
+// beyond that in the exponent.  Scales of K are not negative.  A NaN in V that only some
 // rows of the tile see is taken out and its first token noted for its column; rows that see that token get NaN.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -66,6 +66,12 @@ template <int D> struct Columns {
     }
 };
 
+// The larger of a lane's value and that of lane ^ 32.
+__device__ __forceinline__ float over_halves(float x) {
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
 // A barrier for what is in LDS: global loads stay in flight over it (__syncthreads() waits for them).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -96,7 +102,10 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     if (!locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
             const Sequence s = sequence(p.seq, i);
             return tiles_of<R>(p, s) * chunks_of(s, chunk);
-        }, &b, &rest)) return;
+        }, &b, &rest)) {
+        if (p.split && threadIdx.x == 0) p.splits[blockIdx.x].parts = 0;
+        return;
+    }
     b = __builtin_amdgcn_readfirstlane(b);
     rest = __builtin_amdgcn_readfirstlane(rest);
     const Sequence s = sequence(p.seq, b);
@@ -109,6 +118,8 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     const int64_t from64 = (int64_t)ch * chunk;
     const int end = from64 + chunk < last ? (int)from64 + chunk : last, from = from64 < end ? (int)from64 : end;
     const int plain = all < end ? all : end; // all rows see the tokens below
+    if (p.split && tid == 0)
+        p.splits[blockIdx.x] = {chunks > 1 && ch == 0 ? (int)chunks : 0, (int)slot, (int)slot + 1, 1, s.first, (int)tile * R, rows, 0};
     // this wave's and this lane's rows
     const int w0 = 32 * wave, row = w0 + i;
     const bool works = w0 < rows;
@@ -117,12 +128,14 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     const int tok = token_of(real ? row : 0), head = (int)(tile * R) + (real ? row : 0) - tok * p.group;
     const int limit = real ? limit_of(p, s, tok) : s.seen;
     v8 q[K::steps];
+    const float c_abs = fabsf(p.c); // (a negative scale turns the queries' signs)
+    const uint32_t sign = p.c < 0.f ? 0x80008000u : 0u;
     {
         const T *src = (const T *)p.q + (int64_t)(s.first + tok) * p.qt + (int64_t)(h * p.group + head) * p.qh + 8 * g;
 #pragma unroll
         for (int c = 0; c < K::steps; ++c) {
             const u32x4 w = *(const u32x4 *)(src + 16 * c);
-            q[c] = __builtin_bit_cast(v8, real ? w : u32x4{0, 0, 0, 0});
+            q[c] = __builtin_bit_cast(v8, real ? w ^ sign : u32x4{0, 0, 0, 0});
         }
     }
     for (int d = tid; d < D; d += K::threads) first_nan[d] = 0x7fffffff;
@@ -229,15 +242,10 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
                 *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
         }
         if (tid < K::groups) {
-            f32x4 x = {there ? p.c * ks : 0.f, there ? 0.f : -INFINITY, 1.f, 0.f};
-            vs = there ? vs : 1.f;
-            if (K::f16) {
-                const float v = fminf(fmaxf(vs, 0x1p-60f), 0x1p60f);
-                x[1] += __builtin_amdgcn_logf(v);
-                x[2] = 1.0f / v;
-            } else { // what V's scale is beyond its power of two
-                x[2] = __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
-            }
+            // what of V's scale is not in V goes to the exponent: all of it (fp16), or what it is beyond its power of two
+            const float v = !there ? 1.f : K::f16 ? fminf(fmaxf(vs, 0x1p-60f), 0x1p60f) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
+            // (a factor of zero would make NaN of the -inf that hides a token)
+            const f32x4 x = {!there ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, there ? __builtin_amdgcn_logf(v) : -INFINITY, 1.0f / v, 0.f};
             *(f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * tid) = x;
         }
     };
@@ -262,23 +270,23 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         f32x4 par[K::groups];
 #pragma unroll
         for (int k = 0; k < K::groups; ++k) par[k] = *(const f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * k);
-        float most = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < K::blocks; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sc[j][r] = __builtin_fmaf(sc[j][r], par[2 * j + (r >> 3)][0], par[2 * j + (r >> 3)][1]);
-        if (t0 + TN > wave_all) {
+        if (t0 + TN > wave_all) { // (what is hidden is below everything under either sign of the scale)
             const int room = limit - t0 - 4 * g;
 #pragma unroll
             for (int j = 0; j < K::blocks; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sc[j][r] = 32 * j + 8 * (r >> 2) + (r & 3) < room ? sc[j][r] : -INFINITY;
         }
+        // the largest of each 16 tokens, whose factor is one and not negative, then of all of them
+        float most = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < K::blocks; ++j)
+        for (int k = 0; k < K::groups; ++k) {
+            float x = fmaxf(sc[k / 2][8 * (k & 1)], sc[k / 2][8 * (k & 1) + 1]);
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) most = fmaxf(fmaxf(sc[j][r], sc[j][r + 1]), most);
-        most = fmaxf(most, __shfl_xor(most, 32));
+            for (int r = 2; r < 8; r += 2) x = fmaxf(fmaxf(sc[k / 2][8 * (k & 1) + r], sc[k / 2][8 * (k & 1) + r + 1]), x);
+            most = fmaxf(most, __builtin_fmaf(x, par[k][0], par[k][1]));
+        }
+        most = over_halves(most);
         if (__any(most > m + 8.f)) {
             const float top = fmaxf(most, m), by = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
             m = top;
@@ -289,30 +297,17 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
                 for (int r = 0; r < 16; ++r) o[c][r] *= by;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        v8 pw[2 * K::blocks];
+        v8 pw[K::groups];
 #pragma unroll
-        for (int j = 0; j < K::blocks; ++j)
+        for (int k = 0; k < K::groups; ++k) {
+            const float add = par[k][1] - ref;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float w = __builtin_amdgcn_exp2f(sc[j][r] - ref);
-                l = K::f16 ? __builtin_fmaf(w, par[2 * j + (r >> 3)][2], l) : l + w;
-                sc[j][r] = w;
-            }
-        if constexpr (!K::f16) {
-            float over = 0.f;
-#pragma unroll
-            for (int k = 0; k < K::groups; ++k) over += par[k][2] - 1.f;
-            if (__builtin_amdgcn_readfirstlane(__float_as_uint(over)) != 0) {
-#pragma unroll
-                for (int j = 0; j < K::blocks; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sc[j][r] *= par[2 * j + (r >> 3)][2];
+            for (int r = 0; r < 8; ++r) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][8 * (k & 1) + r], par[k][0], add));
+                l = __builtin_fmaf(w, par[k][2], l);
+                pw[k][r] = (T)w;
             }
         }
-#pragma unroll
-        for (int j = 0; j < K::blocks; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) pw[2 * j + (r >> 3)][r & 7] = (T)sc[j][r];
         const uint8_t *vp = buf + K::k_bytes + i * K::v_pitch + 16 * g;
 #pragma unroll
         for (int c = 0; c < K::operands; ++c)
@@ -349,7 +344,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     if (!real) return;
     const bool whole = chunks == 1;
     const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.0f / l;
-    const int64_t place = ((int64_t)(slot - rest + tile * chunks + ch) * p.heads + h) * p.part_rows + row; // (slots count tiles upwards)
+    const int64_t place = ((int64_t)slot * p.heads + h) * p.part_rows + row;
     if (!whole && g == 0) { p.part_ml[2 * place] = m; p.part_ml[2 * place + 1] = l; }
     T *const out = (T *)p.out + (int64_t)(s.first + tok) * p.ot + (int64_t)(h * p.group + head) * p.oh;
     // n neighbouring columns from d, their products o[c0 + x / per] at register r0 + x % per

@@ -14,28 +14,31 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a tile's parts, for `at_once` rows of a tile and head; part i stands at
-// place(i) of the workspace.  A row's lanes take four elements of every slices-th part each; their sums are added in that order.
-template <typename T, int R, typename F>
-__device__ __forceinline__ void join(const Params &p, const Sequence &s, int h, uint32_t tile, int row0, int at_once, int size, int parts, F place) {
-    const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
-    if (rows <= row0) return;
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts of a tile, for `at_once` of its rows.  A row's lanes take four
+// elements of every slices-th part each; their sums are added in that order.
+template <typename T> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
+    const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once, block = blockIdx.x / groups;
+    const int row0 = (int)(blockIdx.x - block * groups) * at_once, h = (int)(block % (uint32_t)p.heads);
+    const Split t = p.splits[block];
+    if (t.parts == 0 || t.rows <= row0) return;
     const int quads = size / 4, slices = 256 / (quads * at_once);
     const int unit = threadIdx.x / quads, slice = unit / at_once, row = at_once == 1 ? row0 : row0 + unit - slice * at_once, d = 4 * (threadIdx.x - unit * quads);
-    const bool works = slice < slices && row < rows;
-    const auto at = [&](int i) __attribute__((always_inline)) { return ((int64_t)place(i) * p.heads + h) * p.part_rows + row; };
+    const bool works = slice < slices && row < t.rows;
+    const auto at = [&](int i) __attribute__((always_inline)) {
+        return ((int64_t)(i == 0 ? t.first : t.second + (i - 1) * t.step) * p.heads + h) * p.part_rows + row;
+    };
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     if (at_once == 1) { // one row for the whole wave
-        for (int i = threadIdx.x & 63; i < parts; i += 64) m = fmaxf(m, p.part_ml[2 * at(i)]);
+        for (int i = threadIdx.x & 63; i < t.parts; i += 64) m = fmaxf(m, p.part_ml[2 * at(i)]);
         for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
     } else if (works) {
 #pragma unroll 4
-        for (int i = 0; i < parts; ++i) m = fmaxf(m, p.part_ml[2 * at(i)]);
+        for (int i = 0; i < t.parts; ++i) m = fmaxf(m, p.part_ml[2 * at(i)]);
     }
     if (works) {
 #pragma unroll 4
-        for (int i = slice; i < parts; i += slices) {
+        for (int i = slice; i < t.parts; i += slices) {
             const int64_t a = at(i);
             const float mi = p.part_ml[2 * a], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m); // (nothing seen: zeros, or NaN)
             l += p.part_ml[2 * a + 1] * by;
@@ -53,70 +56,12 @@ __device__ __forceinline__ void join(const Params &p, const Sequence &s, int h, 
         l += sum[threadIdx.x + i * at_once * quads];
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    const int r = (int)tile * R + row, t = (int)quotient(r, p.group_magic, p.group_shift), head = r - t * p.group;
+    const int r = t.row + row, token = (int)quotient(r, p.group_magic, p.group_shift), head = r - token * p.group;
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (T)(o[e] * inv);
-    *(T4 *)((T *)p.out + (int64_t)(s.first + t) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
-}
-
-// Many rows: a block looks after at_once rows of a tile, whatever its chunks.
-template <typename T, int R> __global__ __launch_bounds__(256) void join_chunks_kernel(const Params p, int size, int at_once) {
-    const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once;
-    const uint32_t tile_of = blockIdx.x / groups, number = tile_of / (uint32_t)p.heads;
-    const int row0 = (int)(blockIdx.x - tile_of * groups) * at_once, h = (int)(tile_of - number * p.heads);
-    const int chunk = chunk_of<R>(p);
-    int b;
-    uint32_t tile;
-    if (!locate(number, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
-    const Sequence s = sequence(p.seq, b);
-    const int chunks = (int)chunks_of(s, chunk);
-    if (chunks == 1) return;
-    uint32_t slot = 0; // slots before this sequence's
-    for (int i = threadIdx.x & 63; i < b; i += 64) {
-        const Sequence o = sequence(p.seq, i);
-        slot += tiles_of<R>(p, o) * chunks_of(o, chunk);
-    }
-    slot = (uint32_t)wave_sum(slot) + tile * chunks;
-    join<T, R>(p, s, h, tile, row0, at_once, size, chunks, [&](int i) __attribute__((always_inline)) { return slot + i; });
-}
-
-// Few rows: a block looks after at_once rows of a tile.  BY_TILE: tile number j; else the tile that cut j + 1 (between pieces j
-// and j + 1) goes through, if no cut before it does: whichever are fewer.
-template <typename T, int R, bool BY_TILE> __global__ __launch_bounds__(256) void join_pieces_kernel(const Params p, int size, int at_once) {
-    const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once;
-    const uint32_t number = blockIdx.x / groups;
-    uint32_t j = number / (uint32_t)p.heads, total, rest, tile, x;
-    const int row0 = (int)(blockIdx.x - number * groups) * at_once, h = (int)(number - j * p.heads);
-    const uint32_t piece = piece_of<R>(p, &total);
-    int b;
-    if (BY_TILE) {
-        if (!locate(j, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &tile)) return;
-    } else {
-        if (++j * piece >= total || !locate_unit<R>(p, j * piece, &b, &rest)) return;
-    }
-    const Sequence s = sequence(p.seq, b);
-    const uint32_t units = units_of(s);
-    if (BY_TILE) { // its first cut behind a token
-        uint32_t before = 0;
-        for (int i = threadIdx.x & 63; i < b; i += 64) {
-            const Sequence o = sequence(p.seq, i);
-            before += tiles_of<R>(p, o) * units_of(o);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
-        before += tile * units;
-        j = (before + 1) / piece + 1;
-        x = j * piece - before;
-        if (x >= units) return;
-    } else {
-        tile = rest / units;
-        x = rest - tile * units;
-        if (x < 2 || x >= piece + 2) return; // no token before the cut; another cut before it
-    }
-    const int parts = 1 + (int)((units - x + piece - 1) / piece);
-    join<T, R>(p, s, h, tile, row0, at_once, size, parts, [&](int i) __attribute__((always_inline)) { return i ? 2 * (j + i - 1) : 2 * j - 1; });
+    *(T4 *)((T *)p.out + (int64_t)(t.token + token) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
 }
 
 struct Plan {
@@ -181,6 +126,7 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     p.k_page = m.k_stride[0]; p.k_head = m.k_stride[1]; p.v_page = m.v_stride[0]; p.v_head = m.v_stride[1];
     p.ks_page = m.k_scale_stride; p.vs_page = m.v_scale_stride;
     p.part = p.part_ml = nullptr;
+    p.splits = nullptr;
     p.c = c->scale * 1.44269504088896341f;
     p.causal = c->causal != 0; p.split = split;
     p.pages = (int32_t)m.pages; p.heads = (int32_t)m.heads; p.group = (int32_t)group;
@@ -191,30 +137,18 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     o->tiles = (unsigned)tiles;
     o->blocks = (unsigned)(slots * m.heads);
     o->places = places * m.heads;
-    if (split) o->workspace = o->places * p.part_rows * (m.size + 2) * 4;
+    if (split) o->workspace = o->places * p.part_rows * (m.size + 2) * 4 + (int64_t)o->blocks * sizeof(Split);
     return MCF_OK;
 }
 
 } // namespace
 
-static int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, void *stream) {
-    const auto run = [&](auto t) {
-        typedef decltype(t) T;
-        // a row a block where a tile has many parts (all lanes share them out), else as many rows as the lanes hold
-        const int at_once = tile_rows <= 64 && p.slots >= 8 * tiles ? 1 : 256 / (size / 4);
-        const unsigned groups = (unsigned)(p.part_rows + at_once - 1) / at_once;
-        const bool by_tile = tiles < p.slots;
-        const dim3 chunks(tiles * p.heads * groups), pieces((by_tile ? tiles : p.slots - 1) * p.heads * groups), block(256);
-        hipStream_t st = (hipStream_t)stream;
-        if (tile_rows == 128) hipLaunchKernelGGL((join_chunks_kernel<T, 128>), chunks, block, 0, st, p, size, at_once);
-        else if (tile_rows == 256) hipLaunchKernelGGL((join_chunks_kernel<T, 256>), chunks, block, 0, st, p, size, at_once);
-        else if (p.slots == 1) return;
-        else if (tile_rows == 16) by_tile ? join_pieces_kernel<T, 16, true><<<pieces, block, 0, st>>>(p, size, at_once) : join_pieces_kernel<T, 16, false><<<pieces, block, 0, st>>>(p, size, at_once);
-        else if (tile_rows == 32) by_tile ? join_pieces_kernel<T, 32, true><<<pieces, block, 0, st>>>(p, size, at_once) : join_pieces_kernel<T, 32, false><<<pieces, block, 0, st>>>(p, size, at_once);
-        else by_tile ? join_pieces_kernel<T, 64, true><<<pieces, block, 0, st>>>(p, size, at_once) : join_pieces_kernel<T, 64, false><<<pieces, block, 0, st>>>(p, size, at_once);
-    };
-    if (dtype == MCF_F16) run((_Float16)0);
-    else run((__bf16)0);
+static int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, unsigned blocks, void *stream) {
+    // a row a block where a tile has many parts (all lanes share them out), else as many rows as the lanes hold
+    const int at_once = tile_rows <= 64 && p.slots >= 8 * tiles ? 1 : 256 / (size / 4);
+    const dim3 grid(blocks * ((p.part_rows + at_once - 1) / at_once)), block(256);
+    if (dtype == MCF_F16) hipLaunchKernelGGL((join_kernel<_Float16>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
+    else hipLaunchKernelGGL((join_kernel<__bf16>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
     return (int)hipGetLastError();
 }
 
@@ -250,13 +184,14 @@ extern "C" int mcf_cache_attention(const mcf_attention_call *c, void *workspace,
     if (l.workspace > 0) {
         p.part = (float *)workspace;
         p.part_ml = p.part + l.places * p.part_rows * c->cache.size;
+        p.splits = (attend::Split *)(p.part_ml + 2 * l.places * p.part_rows);
     }
     const int size = (int)c->cache.size;
     const bool f16 = c->dtype == MCF_F16;
     int err;
     if (l.tile_rows <= 64) err = (f16 ? attend::launch_rows_f16 : attend::launch_rows_bf16)(p, size, l.tile_rows / 16, l.blocks, stream);
     else err = (f16 ? attend::launch_tiles_f16 : attend::launch_tiles_bf16)(p, size, l.tile_rows / 32, l.blocks, stream);
-    if (err == hipSuccess && l.workspace > 0) err = attend::launch_join(p, c->dtype, size, l.tile_rows, l.tiles, stream);
+    if (err == hipSuccess && l.workspace > 0 && p.slots > 1) err = attend::launch_join(p, c->dtype, size, l.tile_rows, l.tiles, l.blocks, stream);
     if (err == hipSuccess) return MCF_OK;
     set_last_error(hipGetErrorString((hipError_t)err));
     return MCF_ELAUNCH;
