@@ -15,8 +15,8 @@
 // times tokens
 //     chunk = W / (S - T), rounded up      =>      sum over tiles of ceil(tokens / chunk) <= W / chunk + T <= S.
 //
-// The block that leaves a tile's first part also notes where the others will stand (Split), and a second kernel, a block for each
-// that there was, joins them.
+// The block that leaves a tile's first part also notes where the others will stand (Split), and a second kernel joins them: a block
+// for each block that there was, or, where tiles are fewer (and sequences no more than a wave finds the number of a tile for), for each tile.
 #pragma once
 #include "sequences.hpp"
 
@@ -45,9 +45,10 @@ struct Params {
     int64_t ks_page, vs_page;
     float *part;     // [places * heads][part_rows][size]: what a part leaves
     float *part_ml;  // [places * heads][part_rows][2]: its reference exponent and its sum
-    Split *splits;   // [slots * heads]: the tile whose first part the block wrote
+    Split *splits;   // [slots * heads]: the tile whose first part the block wrote; with by_tile [tiles * heads]: every tile's
+    int32_t *tiles;  // with by_tile: how many there are
     float c;         // scale * log2(e)
-    int32_t causal, split;
+    int32_t causal, split, by_tile;
     int32_t pages, heads, group, page_log;
     int32_t part_rows;
     uint32_t slots; // blocks of a head (few rows, split: pieces)
@@ -71,7 +72,8 @@ template <int R> __device__ __forceinline__ uint32_t tiles_of(const Params &p, c
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
 // Piece j of the line: its first unit and the one behind it, and where the first lies: the sequence and the units before it there.
 // False: beyond the line.  Up to 64 sequences are read once, a lane each (two passes over more of them).
-template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uint32_t j, uint32_t *piece, uint32_t *at, uint32_t *end, int *b, uint32_t *rest, Sequence *s) {
+template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uint32_t j, uint32_t *piece, uint32_t *at, uint32_t *end, int *b, uint32_t *rest, Sequence *s,
+                                           uint32_t *tiles_before, uint32_t *all_tiles) {
     const int lane = threadIdx.x & 63;
     const auto units = [&](const Sequence &q) __attribute__((always_inline)) { return tiles_of<R>(p, q) * units_of(q); };
     const auto cut = [&](uint32_t total) __attribute__((always_inline)) {
@@ -84,17 +86,19 @@ template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uin
     if (p.seq.batch <= 64) {
         Sequence q = {0, 0, 0, 0};
         if (lane < p.seq.batch) q = sequence(p.seq, lane);
-        const uint32_t n = units(q);
-        uint32_t upto = n;
+        const uint32_t n = units(q), tiles = tiles_of<R>(p, q);
+        uint32_t upto = n, tiles_upto = tiles;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const uint32_t x = __shfl_up(upto, d);
-            if (lane >= d) upto += x;
+            const uint32_t x = __shfl_up(upto, d), y = __shfl_up(tiles_upto, d);
+            if (lane >= d) { upto += x; tiles_upto += y; }
         }
+        *all_tiles = __builtin_amdgcn_readlane(tiles_upto, 63);
         if (!cut(__builtin_amdgcn_readlane(upto, 63))) return false;
         const int i = __builtin_ctzll(__ballot(*at - (upto - n) < n));
         *b = i;
         *rest = *at - (__builtin_amdgcn_readlane(upto, i) - __builtin_amdgcn_readlane(n, i));
+        *tiles_before = __builtin_amdgcn_readlane(tiles_upto, i) - __builtin_amdgcn_readlane(tiles, i);
         *s = {__builtin_amdgcn_readlane(q.first, i), __builtin_amdgcn_readlane(q.rows, i), __builtin_amdgcn_readlane(q.length, i), __builtin_amdgcn_readlane(q.seen, i)};
         return true;
     }

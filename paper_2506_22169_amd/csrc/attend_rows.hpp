@@ -389,11 +389,12 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribu
     const uint32_t j = blockIdx.x / (uint32_t)p.heads;
     const int h = (int)(blockIdx.x - j * p.heads);
     int b;
-    uint32_t rest, at = 0, end = 1, piece = 1;
+    uint32_t rest, at = 0, end = 1, piece = 1, tiles_before = 0, all_tiles = 0;
     Sequence s;
     Split split = {0, 0, 0, 0, 0, 0, 0, 0};
     if (p.split) {
-        if (!find_piece<R>(p, j, &piece, &at, &end, &b, &rest, &s)) at = end = 0;
+        if (!find_piece<R>(p, j, &piece, &at, &end, &b, &rest, &s, &tiles_before, &all_tiles)) at = end = 0;
+        if (p.by_tile && blockIdx.x == 0 && threadIdx.x == 0) *p.tiles = (int)all_tiles;
     } else { // tile j, as the one unit of a piece
         if (!locate(j, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, sequence(p.seq, i)); }, &b, &rest)) return;
         b = __builtin_amdgcn_readfirstlane(b);
@@ -407,19 +408,22 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribu
             const int from = first_token(x), to = x + n == units ? 0x7fffffff : first_token(x + n);
             const bool whole = from == 0 && x + n == units;
             if (from < to) tile_part<T, D, NB>(p, s, b, h, tile, from, to, whole ? -1 : (int)(2 * j + (from == 0)));
-            if (from == 0 && to > 0 && !whole) { // the first of several parts
+            if (from == 0 && to > 0) { // the first of one or more parts
                 const int rows = s.rows * p.group - (int)tile * R;
-                split = {1 + (int)((units - x - n + piece - 1) / piece), (int)(2 * j + 1), (int)(2 * j + 2), 2, s.first, (int)tile * R, rows < R ? rows : R, 0};
+                const Split first = {whole ? 0 : 1 + (int)((units - x - n + piece - 1) / piece), (int)(2 * j + 1), (int)(2 * j + 2), 2, s.first, (int)tile * R, rows < R ? rows : R, 0};
+                if (!whole) split = first;
+                if (p.by_tile && threadIdx.x == 0) p.splits[(tiles_before + tile) * p.heads + h] = first;
             }
             rest += n;
             at += n;
         }
         if (at >= end) break;
         rest = 0;
+        tiles_before += all / units;
         if (++b >= p.seq.batch) break;
         s = sequence(p.seq, b);
     }
-    if (p.split && threadIdx.x == 0) p.splits[blockIdx.x] = split;
+    if (p.split && !p.by_tile && threadIdx.x == 0) p.splits[blockIdx.x] = split;
 }
 
 template <typename T> int launch_rows(const Params &p, int size, int row_blocks, unsigned blocks, void *stream) {

@@ -19,6 +19,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
     const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once, block = blockIdx.x / groups;
     const int row0 = (int)(blockIdx.x - block * groups) * at_once, h = (int)(block % (uint32_t)p.heads);
+    if (p.by_tile && block >= (uint32_t)(*p.tiles * p.heads)) return;
     const Split t = p.splits[block];
     if (t.parts == 0 || t.rows <= row0) return;
     const int quads = size / 4, slices = 256 / (quads * at_once);
@@ -126,9 +127,9 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     p.k_page = m.k_stride[0]; p.k_head = m.k_stride[1]; p.v_page = m.v_stride[0]; p.v_head = m.v_stride[1];
     p.ks_page = m.k_scale_stride; p.vs_page = m.v_scale_stride;
     p.part = p.part_ml = nullptr;
-    p.splits = nullptr;
+    p.splits = nullptr; p.tiles = nullptr;
     p.c = c->scale * 1.44269504088896341f;
-    p.causal = c->causal != 0; p.split = split;
+    p.causal = c->causal != 0; p.split = split; p.by_tile = split && R <= 64 && batch <= 64 && tiles < slots;
     p.pages = (int32_t)m.pages; p.heads = (int32_t)m.heads; p.group = (int32_t)group;
     p.page_log = m.page_size == 16 ? 4 : m.page_size == 32 ? 5 : m.page_size == 64 ? 6 : 7;
     p.part_rows = c->seq.starts ? R : group < R ? (int)group : R;
@@ -137,7 +138,7 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     o->tiles = (unsigned)tiles;
     o->blocks = (unsigned)(slots * m.heads);
     o->places = places * m.heads;
-    if (split) o->workspace = o->places * p.part_rows * (m.size + 2) * 4 + (int64_t)o->blocks * sizeof(Split);
+    if (split) o->workspace = o->places * p.part_rows * (m.size + 2) * 4 + (int64_t)o->blocks * sizeof(Split) + 16;
     return MCF_OK;
 }
 
@@ -146,7 +147,7 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
 static int launch_join(const Params &p, int dtype, int size, int tile_rows, unsigned tiles, unsigned blocks, void *stream) {
     // a row a block where a tile has many parts (all lanes share them out), else as many rows as the lanes hold
     const int at_once = tile_rows <= 64 && p.slots >= 8 * tiles ? 1 : 256 / (size / 4);
-    const dim3 grid(blocks * ((p.part_rows + at_once - 1) / at_once)), block(256);
+    const dim3 grid((p.by_tile ? tiles * p.heads : blocks) * ((p.part_rows + at_once - 1) / at_once)), block(256);
     if (dtype == MCF_F16) hipLaunchKernelGGL((join_kernel<_Float16>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
     else hipLaunchKernelGGL((join_kernel<__bf16>), grid, block, 0, (hipStream_t)stream, p, size, at_once);
     return (int)hipGetLastError();
@@ -184,7 +185,8 @@ extern "C" int mcf_cache_attention(const mcf_attention_call *c, void *workspace,
     if (l.workspace > 0) {
         p.part = (float *)workspace;
         p.part_ml = p.part + l.places * p.part_rows * c->cache.size;
-        p.splits = (attend::Split *)(p.part_ml + 2 * l.places * p.part_rows);
+        p.tiles = (int32_t *)(p.part_ml + 2 * l.places * p.part_rows);
+        p.splits = (attend::Split *)(p.tiles + 4);
     }
     const int size = (int)c->cache.size;
     const bool f16 = c->dtype == MCF_F16;
