@@ -99,16 +99,13 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     const int chunk = __builtin_amdgcn_readfirstlane(chunk_of<R>(p));
     int b;
     uint32_t rest;
-    if (!locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
-            const Sequence s = sequence(p.seq, i);
-            return tiles_of<R>(p, s) * chunks_of(s, chunk);
-        }, &b, &rest)) {
+    Sequence s;
+    if (!locate_sequence(p.seq, slot, [&](const Sequence &q) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, q) * chunks_of(q, chunk); }, &b, &rest, &s)) {
         if (p.split && threadIdx.x == 0) p.splits[blockIdx.x].parts = 0;
         return;
     }
     b = __builtin_amdgcn_readfirstlane(b);
     rest = __builtin_amdgcn_readfirstlane(rest);
-    const Sequence s = sequence(p.seq, b);
     const uint32_t chunks = chunks_of(s, chunk), at = rest / chunks, ch = rest - at * chunks;
     const uint32_t tile = tiles_of<R>(p, s) - 1 - at; // the last rows, which see most, first
     const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;

@@ -91,9 +91,10 @@ struct Turn {
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+            // (the rounding of each is written out: whoever turns a row gets the same bits)
             const F sn = BACK ? -(F)s[e] : (F)s[e], cs = (F)c[e], t = x[e];
-            x[e] = t * cs - y[e] * sn;
-            y[e] = y[e] * cs + t * sn;
+            x[e] = __builtin_elementwise_fma(t, cs, -(y[e] * sn));
+            y[e] = __builtin_elementwise_fma(y[e], cs, t * sn);
         }
         if (interleaved) {
 #pragma unroll
@@ -117,6 +118,16 @@ template <typename T> __device__ __forceinline__ void load_weight(const void *w,
 #pragma unroll
         for (int e = 0; e < 8; ++e) { wa[e] = (float)a.e[e]; wb[e] = (float)b.e[e]; }
     }
+}
+
+// A row's norm: its elements times 1 / sqrt(mean of squares + eps) and the weights.
+template <int LPR> __device__ __forceinline__ void norm_row(float a[8], float b[8], const float wa[8], const float wb[8], float inv_size, float eps) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(b[e], b[e], __builtin_fmaf(a[e], a[e], sum));
+    const float r = 1.0f / sqrtf(__builtin_fmaf(row_sum<LPR>(sum), inv_size, eps));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { a[e] = a[e] * r * wa[e]; b[e] = b[e] * r * wb[e]; }
 }
 
 // Lanes that a row lies on.

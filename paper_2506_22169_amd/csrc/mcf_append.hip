@@ -2,10 +2,10 @@
 // page and head that tokens go into, rounding to e4m3; and, by further blocks of the same launch, norm and rotation of the
 // queries.
 //
-// A block takes one page and head of K or V: what it needs to know of it (the largest value, the scale so far, the tokens that
+// A block takes one page and head of K and V: what it needs to know of them (the largest values, the scales so far, the tokens that
 // are held) concerns nobody else, so there are no atomics and the result does not depend on any order.  Its lanes keep
 // the page's new values in registers between the search for the largest and the rounding, so that the inputs are read
-// once.  Bound by memory with prompts (2 bytes in, 1 out an element), by the latency of two dependent loads and a launch with single tokens.
+// once, and K and V together keep twice the loads in flight for one search for the sequence.  Bound by memory with prompts (2 bytes in, 1 out an element), by the latency of two dependent loads and a launch with single tokens.
 //
 // Keys are computed in 64 bits: the rounding to e4m3 is a step of 1/16 to 1/8 of a value, and a key that lies next to a border
 // between two steps would otherwise go to either side by the order of the sums, so that the same token appended alone and
@@ -24,7 +24,6 @@ namespace heads {
 namespace {
 
 constexpr float kSmallestScale = 0x1p-100f;
-constexpr int kPasses = 2; // rows of a page that a group of lanes keeps
 
 struct Params {
     Sequences seq;
@@ -41,8 +40,8 @@ struct Params {
     float inv_size;
     int32_t weight_f32, interleaved, size, rotary;
     int32_t pages, k_heads, page_log;
-    uint32_t cache_blocks;      // slots * heads * 2
-    uint32_t q_items, q_heads;
+    uint32_t cache_blocks;      // slots * heads
+    uint32_t q_items, q_heads, q_groups;
     uint32_t heads_magic, q_magic;
     int32_t heads_shift, q_shift;
 };
@@ -97,144 +96,167 @@ __device__ __forceinline__ void key_row(const Params &p, const Unit &u, const fl
     for (int e = 0; e < 8; ++e) { va[e] = (float)xa[e]; vb[e] = (float)xb[e]; }
 }
 
-// One head of one query.
-template <typename T, int LPR> __device__ __forceinline__ void query_row(const Params &p, uint32_t item) {
+// Up to HPG heads of one query (head, head + groups, ...).  What a query reads of its own is asked for before its sequence is known.
+template <typename T, int LPR, int HPG> __device__ __forceinline__ void query_rows(const Params &p, uint32_t item) {
     if (item >= p.q_items) return;
-    const uint32_t t = quotient(item, p.q_magic, p.q_shift), h = item - t * p.q_heads;
+    const uint32_t t = quotient(item, p.q_magic, p.q_shift), first = item - t * p.q_groups;
+    const Unit u(threadIdx.x % LPR, p.size, p.rotary);
+    const T *x = (const T *)p.q + t * p.qt;
+    T *out = (T *)p.q_out + t * p.ot;
+    Chunk<T> a[HPG], c[HPG];
+#pragma unroll
+    for (int j = 0; j < HPG; ++j) {
+        const uint32_t h = first + j * p.q_groups;
+        a[j].bits = c[j].bits = u32x4{0, 0, 0, 0};
+        if (u.there && h < p.q_heads) { a[j].bits = *(const u32x4 *)(x + h * p.qh + u.a); c[j].bits = *(const u32x4 *)(x + h * p.qh + u.b); }
+    }
+    float wa[8], wb[8];
+    if (p.q_weight) load_weight<T>(p.q_weight, p.weight_f32, u, wa, wb);
     const int b = sequence_of_row(p.seq, (int)t);
     if (b < 0) return;
     const Sequence s = sequence(p.seq, b);
-    const Unit u(threadIdx.x % LPR, p.size, p.rotary);
-    const T *x = (const T *)p.q + t * p.qt + h * p.qh;
-    T *out = (T *)p.q_out + t * p.ot + h * p.oh;
-    Chunk<T> a, c;
-    a.bits = c.bits = u32x4{0, 0, 0, 0};
-    if (u.there) { a.bits = *(const u32x4 *)(x + u.a); c.bits = *(const u32x4 *)(x + u.b); }
     Turn turn;
     turn.load(p.cos, p.sin, (int64_t)s.length - s.rows + ((int)t - s.first), p.table_rows, p.rotary, u, p.interleaved);
-    float xa[8], xb[8], sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { xa[e] = (float)a.e[e]; xb[e] = (float)c.e[e]; sum += xa[e] * xa[e] + xb[e] * xb[e]; }
-    if (p.q_weight) {
-        float wa[8], wb[8];
-        load_weight<T>(p.q_weight, p.weight_f32, u, wa, wb);
-        const float r = 1.0f / sqrtf(row_sum<LPR>(sum) * p.inv_size + (float)p.eps);
+    for (int j = 0; j < HPG; ++j) {
+        const uint32_t h = first + j * p.q_groups;
+        float xa[8], xb[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { xa[e] = xa[e] * r * wa[e]; xb[e] = xb[e] * r * wb[e]; }
+        for (int e = 0; e < 8; ++e) { xa[e] = (float)a[j].e[e]; xb[e] = (float)c[j].e[e]; }
+        if (p.q_weight) norm_row<LPR>(xa, xb, wa, wb, p.inv_size, (float)p.eps);
+        if (u.turns) turn.turn<false>(xa, xb, p.interleaved);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { a[j].e[e] = (T)xa[e]; c[j].e[e] = (T)xb[e]; }
+        if (u.there && h < p.q_heads) { *(u32x4 *)(out + h * p.oh + u.a) = a[j].bits; *(u32x4 *)(out + h * p.oh + u.b) = c[j].bits; }
     }
-    if (u.turns) turn.turn<false>(xa, xb, p.interleaved);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { a.e[e] = (T)xa[e]; c.e[e] = (T)xb[e]; }
-    if (u.there) { *(u32x4 *)(out + u.a) = a.bits; *(u32x4 *)(out + u.b) = c.bits; }
 }
 
-template <typename T, int LPR> __global__ __launch_bounds__(1024) void append_kernel(const Params p) {
+// PASSES: places of a page that a group of lanes looks after; HPG: heads of a query that go together.
+template <typename T, int LPR, int PASSES, int HPG> __global__ __launch_bounds__(1024) void append_kernel(const Params p) {
     if (blockIdx.x >= p.cache_blocks) {
-        query_row<T, LPR>(p, (blockIdx.x - p.cache_blocks) * (blockDim.x / LPR) + threadIdx.x / LPR);
+        query_rows<T, LPR, HPG>(p, (blockIdx.x - p.cache_blocks) * (blockDim.x / LPR) + threadIdx.x / LPR);
         return;
     }
     const int page_size = 1 << p.page_log;
-    const bool is_v = blockIdx.x & 1;
-    const uint32_t sh = blockIdx.x >> 1, slot = quotient(sh, p.heads_magic, p.heads_shift), h = sh - slot * p.k_heads;
-    int b = (int)slot;
-    uint32_t nth = 0;
+    const uint32_t slot = quotient(blockIdx.x, p.heads_magic, p.heads_shift), h = blockIdx.x - slot * p.k_heads;
     const auto range = [&](const Sequence &s, int &lo, int &hi) __attribute__((always_inline)) { // places that the new tokens have
         lo = s.length > s.rows ? s.length - s.rows : 0;
-        hi = s.seen;
+        hi = s.rows > 0 ? s.seen : 0;
     };
+    int b = (int)slot;
+    uint32_t nth = 0;
+    Sequence s;
     if (p.seq.starts) {
-        const bool found = locate(slot, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t {
-            int lo, hi;
-            range(sequence(p.seq, i), lo, hi);
-            return hi > lo ? ((hi - 1) >> p.page_log) - (lo >> p.page_log) + 1 : 0;
-        }, &b, &nth);
-        if (!found) return;
+        if (!locate_sequence(p.seq, slot, [&](const Sequence &q) __attribute__((always_inline)) -> uint32_t {
+                int lo, hi;
+                range(q, lo, hi);
+                return hi > lo ? ((hi - 1) >> p.page_log) - (lo >> p.page_log) + 1 : 0;
+            }, &b, &nth, &s)) return;
+    } else {
+        s = sequence(p.seq, b);
     }
-    const Sequence s = sequence(p.seq, b);
     int lo, hi;
     range(s, lo, hi);
-    if (s.rows == 0 || hi <= lo) return;
+    if (hi <= lo) return;
     const int column = (lo >> p.page_log) + (int)nth;
-    const int id = p.seq.table[b * p.seq.table_stride + column];
-    if (id < 0 || id >= p.pages) return;
+    const int id = p.seq.table[b * p.seq.table_stride + column]; // (looked at when the values are on their way)
     const int base = column << p.page_log;
     const int s0 = lo > base ? lo - base : 0, s1 = hi - base < page_size ? hi - base : page_size; // new places of the page
-    float *const scale = p.scale[is_v] + id * p.scale_stride[is_v] + h;
-    uint8_t *const page = p.page[is_v] + id * p.page_stride[is_v] + h * p.head_stride[is_v];
-    const float old = *scale;
     const Unit u(threadIdx.x % LPR, p.size, p.rotary);
     const int at_once = blockDim.x / LPR, group = threadIdx.x / LPR;
-    const T *const x = (const T *)p.x[is_v] + h * p.xh[is_v];
-    float va[kPasses][8], vb[kPasses][8], wa[8], wb[8], most = 0.f;
-    if (!is_v && p.k_weight) load_weight<T>(p.k_weight, p.weight_f32, u, wa, wb);
+    Chunk<T> a[2][PASSES], c[2][PASSES];
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int place = group + i * at_once;
-        Chunk<T> a, c;
-        a.bits = c.bits = u32x4{0, 0, 0, 0};
-        if (place >= s0 && place < s1 && u.there) {
-            const int64_t t = s.first + (base + place - (s.length - s.rows)); // its row
-            a.bits = *(const u32x4 *)(x + t * p.xt[is_v] + u.a);
-            c.bits = *(const u32x4 *)(x + t * p.xt[is_v] + u.b);
+    for (int i = 0; i < PASSES; ++i) {
+        const int place = s0 + group + i * at_once;
+        const int64_t t = s.first + (base + place - (s.length - s.rows)); // its row
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            a[v][i].bits = c[v][i].bits = u32x4{0, 0, 0, 0};
+            if (place < s1 && u.there) {
+                const T *const x = (const T *)p.x[v] + t * p.xt[v] + h * p.xh[v];
+                a[v][i].bits = *(const u32x4 *)(x + u.a);
+                c[v][i].bits = *(const u32x4 *)(x + u.b);
+            }
         }
-        if (!is_v && (p.k_weight || p.rotary)) {
+    }
+    if (id < 0 || id >= p.pages) return;
+    float old[2];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) old[v] = p.scale[v][id * p.scale_stride[v] + h];
+    float va[2][PASSES][8], vb[2][PASSES][8], wa[8], wb[8], most[2] = {0.f, 0.f};
+    if (p.k_weight) load_weight<T>(p.k_weight, p.weight_f32, u, wa, wb);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int place = s0 + group + i * at_once;
+        if (p.k_weight || p.rotary) {
             Turn turn;
             turn.load(p.cos, p.sin, base + place, p.table_rows, p.rotary, u, p.interleaved);
-            key_row<T, LPR>(p, u, wa, wb, turn, a, c, va[i], vb[i]);
+            key_row<T, LPR>(p, u, wa, wb, turn, a[0][i], c[0][i], va[0][i], vb[0][i]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { va[i][e] = (float)a.e[e]; vb[i][e] = (float)c.e[e]; }
+            for (int e = 0; e < 8; ++e) { va[0][i][e] = (float)a[0][i].e[e]; vb[0][i][e] = (float)c[0][i].e[e]; }
         }
-        // (the places that are not new have values too where a position is beyond the tables)
-        const bool counts = place >= s0 && place < s1;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float *const v[2] = {&va[i][e], &vb[i][e]};
-            for (float *y : v) {
-                const bool finite = fabsf(*y) < INFINITY;
-                if (!finite) *y = __builtin_nanf("");
-                most = fmaxf(most, finite && counts ? fabsf(*y) : 0.f);
+        for (int e = 0; e < 8; ++e) { va[1][i][e] = (float)a[1][i].e[e]; vb[1][i][e] = (float)c[1][i].e[e]; }
+        // (places that are not new have values too where a position is beyond the tables)
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float *const both[2] = {&va[v][i][e], &vb[v][i][e]};
+                for (float *y : both) {
+                    const bool finite = fabsf(*y) < INFINITY;
+                    if (!finite) *y = __builtin_nanf("");
+                    most[v] = fmaxf(most[v], finite && place < s1 ? fabsf(*y) : 0.f);
+                }
             }
+    }
+    most[0] = wave_max(most[0]);
+    most[1] = wave_max(most[1]);
+    if (blockDim.x > 64) {
+        __shared__ float part[2][16];
+        if ((threadIdx.x & 63) < 2) part[threadIdx.x & 1][threadIdx.x >> 6] = threadIdx.x & 1 ? most[1] : most[0];
+        __syncthreads();
+        for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+            most[0] = fmaxf(most[0], part[0][w]);
+            most[1] = fmaxf(most[1], part[1][w]);
         }
     }
-    most = wave_max(most);
-    if (blockDim.x > 64) {
-        __shared__ float part[16];
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-        __syncthreads();
-        for (int w = 0; w < (int)(blockDim.x >> 6); ++w) most = fmaxf(most, part[w]);
-    }
-    float now = scale_of(most);
-    if (s0 > 0) now = fmaxf(now, old);
-    const float inv = 1.0f / now;
-    const bool grows = s0 > 0 && now != old;
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int place = group + i * at_once;
-        uint8_t *const to = page + place * p.size;
-        if (!u.there) continue;
-        if (place >= s0 && place < s1) {
-            u32x2 a, c;
+    for (int v = 0; v < 2; ++v) {
+        uint8_t *const page = p.page[v] + id * p.page_stride[v] + h * p.head_stride[v];
+        float now = scale_of(most[v]);
+        if (s0 > 0) now = fmaxf(now, old[v]);
+        const float inv = 1.0f / now;
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int place = s0 + group + i * at_once;
+            if (place >= s1 || !u.there) continue;
+            uint8_t *const to = page + place * p.size;
+            u32x2 x, y;
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
-                a[d] = pack4(va[i][4 * d] * inv, va[i][4 * d + 1] * inv, va[i][4 * d + 2] * inv, va[i][4 * d + 3] * inv);
-                c[d] = pack4(vb[i][4 * d] * inv, vb[i][4 * d + 1] * inv, vb[i][4 * d + 2] * inv, vb[i][4 * d + 3] * inv);
+                x[d] = pack4(va[v][i][4 * d] * inv, va[v][i][4 * d + 1] * inv, va[v][i][4 * d + 2] * inv, va[v][i][4 * d + 3] * inv);
+                y[d] = pack4(vb[v][i][4 * d] * inv, vb[v][i][4 * d + 1] * inv, vb[v][i][4 * d + 2] * inv, vb[v][i][4 * d + 3] * inv);
             }
-            *(u32x2 *)(to + u.a) = a;
-            *(u32x2 *)(to + u.b) = c;
-        } else if (grows && place < s0) {
-            rescale(to + u.a, old * inv);
-            rescale(to + u.b, old * inv);
+            *(u32x2 *)(to + u.a) = x;
+            *(u32x2 *)(to + u.b) = y;
         }
+        if (s0 > 0 && now != old[v] && u.there) {
+            for (int place = group; place < s0; place += at_once) {
+                rescale(page + place * p.size + u.a, old[v] * inv);
+                rescale(page + place * p.size + u.b, old[v] * inv);
+            }
+        }
+        if (threadIdx.x == 0) p.scale[v][id * p.scale_stride[v] + h] = now;
     }
-    if (threadIdx.x == 0) *scale = now;
 }
 
 } // namespace
 } // namespace heads
 
 // Checks a call and lays it out; *blocks = 0: nothing to do.  MCF_OK or an error status.
-static int plan_append(const mcf_append_call *c, heads::Params *p, unsigned *blocks, unsigned *threads) {
+static int plan_append(const mcf_append_call *c, heads::Params *p, unsigned *blocks, unsigned *threads, int *passes, int *hpg) {
     set_last_error("");
     if (!c) return MCF_EINVAL;
     if (c->dtype != MCF_F16 && c->dtype != MCF_BF16) return MCF_EUNSUPPORTED;
@@ -257,9 +279,15 @@ static int plan_append(const mcf_append_call *c, heads::Params *p, unsigned *blo
     if (slots > tokens) slots = tokens;
     if (m.pages == 0) slots = 0;
     const int lanes = heads::row_lanes(m.size);
-    int64_t lanes_needed = m.page_size * lanes / heads::kPasses;
-    *threads = lanes_needed < 64 ? 64u : (unsigned)lanes_needed;
-    const int64_t cache_blocks = slots * m.heads * 2, q_items = tokens * c->q_heads, q_blocks = (q_items + *threads / lanes - 1) / (*threads / lanes);
+    // the new places of a page side by side in a block (one without starts), two of them a lane where they are more than it holds
+    const int64_t most_places = c->seq.starts ? m.page_size : 1;
+    *passes = most_places * lanes > 1024 ? 2 : 1;
+    const int64_t page_lanes = most_places * lanes / *passes;
+    *threads = page_lanes < 64 ? 64u : (unsigned)page_lanes;
+    // heads of a query share its cosines and sines: four of them together where that leaves eight waves a compute unit
+    *hpg = tokens * c->q_heads * lanes / 64 >= 4 * 8 * kComputeUnits ? 4 : 1;
+    const int64_t q_groups = (c->q_heads + *hpg - 1) / *hpg, per_block = *threads / lanes;
+    const int64_t cache_blocks = slots * m.heads, q_items = tokens * q_groups, q_blocks = (q_items + per_block - 1) / per_block;
     if (slots * m.heads >= 1ll << 30 || q_items >= 1ll << 31 || (cache_blocks + q_blocks) * *threads >= (1ll << 32) - 65536) {
         set_last_error("too many rows for one call");
         return MCF_EUNSUPPORTED;
@@ -282,16 +310,17 @@ static int plan_append(const mcf_append_call *c, heads::Params *p, unsigned *blo
     p->size = (int32_t)m.size; p->rotary = (int32_t)c->rotary;
     p->pages = (int32_t)m.pages; p->k_heads = (int32_t)m.heads;
     p->page_log = m.page_size == 16 ? 4 : m.page_size == 32 ? 5 : m.page_size == 64 ? 6 : 7;
-    p->cache_blocks = (uint32_t)cache_blocks; p->q_items = (uint32_t)q_items; p->q_heads = (uint32_t)c->q_heads;
+    p->cache_blocks = (uint32_t)cache_blocks; p->q_items = (uint32_t)q_items; p->q_heads = (uint32_t)c->q_heads; p->q_groups = (uint32_t)q_groups;
     division_magic((uint32_t)m.heads, &p->heads_magic, &p->heads_shift);
-    division_magic((uint32_t)c->q_heads, &p->q_magic, &p->q_shift);
+    division_magic((uint32_t)q_groups, &p->q_magic, &p->q_shift);
     return MCF_OK;
 }
 
 int check_append(const mcf_append_call *c) {
     heads::Params p;
     unsigned blocks, threads;
-    return plan_append(c, &p, &blocks, &threads);
+    int passes, hpg;
+    return plan_append(c, &p, &blocks, &threads, &passes, &hpg);
 }
 
 } // namespace mcf
@@ -301,17 +330,31 @@ using namespace mcf;
 extern "C" int mcf_cache_append(const mcf_append_call *c, void *stream) {
     heads::Params p;
     unsigned blocks, threads;
-    const int st = plan_append(c, &p, &blocks, &threads);
+    int passes, hpg;
+    const int st = plan_append(c, &p, &blocks, &threads, &passes, &hpg);
     if (st != MCF_OK || blocks == 0) return st;
-    const auto run = [&](auto t) {
+    const auto run = [&](auto t, auto lanes) {
         typedef decltype(t) T;
-        const int lanes = heads::row_lanes(p.size);
-        if (lanes == 4) hipLaunchKernelGGL((heads::append_kernel<T, 4>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
-        else if (lanes == 8) hipLaunchKernelGGL((heads::append_kernel<T, 8>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
-        else hipLaunchKernelGGL((heads::append_kernel<T, 16>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
+        constexpr int L = decltype(lanes)::value;
+        const auto go = [&](auto n, auto g) {
+            hipLaunchKernelGGL((heads::append_kernel<T, L, decltype(n)::value, decltype(g)::value>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, p);
+        };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        if constexpr (L == 16) { // (rows of fewer lanes fit a block)
+            if (passes == 2) { hpg == 4 ? go(two, four) : go(two, one); return; }
+        }
+        hpg == 4 ? go(one, four) : go(one, one);
     };
-    if (c->dtype == MCF_F16) run((_Float16)0);
-    else run((__bf16)0);
+    const auto with = [&](auto t) {
+        const int lanes = heads::row_lanes(p.size);
+        if (lanes == 4) run(t, std::integral_constant<int, 4>());
+        else if (lanes == 8) run(t, std::integral_constant<int, 8>());
+        else run(t, std::integral_constant<int, 16>());
+    };
+    if (c->dtype == MCF_F16) with((_Float16)0);
+    else with((__bf16)0);
     const hipError_t err = hipGetLastError();
     if (err == hipSuccess) return MCF_OK;
     set_last_error(hipGetErrorString(err));

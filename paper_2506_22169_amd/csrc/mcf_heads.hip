@@ -78,14 +78,10 @@ template <typename T, int LPR, int HPG> __global__ __launch_bounds__(256) void r
 #pragma unroll
     for (int j = 0; j < HPG; ++j) {
         const int h = first + j * step;
-        float xa[8], xb[8], sum = 0.f;
+        float xa[8], xb[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { xa[e] = (float)a[j].e[e]; xb[e] = (float)c[j].e[e]; sum += xa[e] * xa[e] + xb[e] * xb[e]; }
-        if (w) {
-            const float r = 1.0f / sqrtf(row_sum<LPR>(sum) * p.inv_size + p.eps);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { xa[e] = xa[e] * r * wa[e]; xb[e] = xb[e] * r * wb[e]; }
-        }
+        for (int e = 0; e < 8; ++e) { xa[e] = (float)a[j].e[e]; xb[e] = (float)c[j].e[e]; }
+        if (w) norm_row<LPR>(xa, xb, wa, wb, p.inv_size, p.eps);
         if (u.turns) turn.turn<false>(xa, xb, p.interleaved);
 #pragma unroll
         for (int e = 0; e < 8; ++e) { a[j].e[e] = (T)xa[e]; c[j].e[e] = (T)xb[e]; }

@@ -64,6 +64,33 @@ template <typename F> __device__ __forceinline__ bool locate(uint32_t slot, int 
     return false;
 }
 
+// The same with the sequence itself, of which up to 64 are read once.
+template <typename F> __device__ __forceinline__ bool locate_sequence(const Sequences &all, uint32_t slot, F count, int *b, uint32_t *rest, Sequence *s) {
+    if (all.batch > 64) {
+        if (!locate(slot, all.batch, [&](int i) __attribute__((always_inline)) { return count(sequence(all, i)); }, b, rest)) return false;
+        *b = __builtin_amdgcn_readfirstlane(*b);
+        *s = sequence(all, *b);
+        return true;
+    }
+    const int lane = threadIdx.x & 63;
+    Sequence q = {0, 0, 0, 0};
+    if (lane < all.batch) q = sequence(all, lane);
+    const uint32_t n = count(q);
+    uint32_t upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t x = __shfl_up(upto, d);
+        if (lane >= d) upto += x;
+    }
+    const uint64_t hit = __ballot(slot - (upto - n) < n);
+    if (!hit) return false;
+    const int i = __builtin_ctzll(hit);
+    *b = i;
+    *rest = slot - (__builtin_amdgcn_readlane(upto, i) - __builtin_amdgcn_readlane(n, i));
+    *s = {__builtin_amdgcn_readlane(q.first, i), __builtin_amdgcn_readlane(q.rows, i), __builtin_amdgcn_readlane(q.length, i), __builtin_amdgcn_readlane(q.seen, i)};
+    return true;
+}
+
 // The sequence that row t belongs to (starts ascending), -1: none.
 __device__ __forceinline__ int sequence_of_row(const Sequences &s, int t) {
     if (!s.starts) return t < s.batch ? t : -1;
