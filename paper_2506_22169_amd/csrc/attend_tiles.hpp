@@ -1,6 +1,6 @@
 // Attention of many rows over the paged cache of 8 bits: prompts and pieces of prompts (attend.hpp says how the work is laid out).
 //
-// A block of W waves takes a tile of 32 W rows, each wave 32 of them, and goes over the tokens 64 (size > 128: 32) at a time:
+// A block of W waves takes a tile of 32 W rows, each wave 32 of them, and goes over the tokens TN at a time:
 //     S^T = K Q^T, O^T += V^T P^T   v_mfma 32x32x16; a lane holds one row, so that its softmax needs one exchange (with lane ^ 32),
 //     and S^T's result layout is P^T's operand as it is, with the tokens counted in that order.
 // Bound by the matrix instructions and, next to them, by the vector instructions of the softmax and the LDS reads of their
@@ -78,11 +78,11 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 template <typename T, int D, int WAVES> struct Tiles {
     typedef typename Wide<T>::v8 v8;
     static constexpr bool f16 = std::is_same<T, _Float16>::value;
-    static constexpr int TN = D <= 128 ? 64 : 32, R = 32 * WAVES, threads = 64 * WAVES;
+    static constexpr int TN = D <= 96 ? 128 : D <= 128 ? 64 : 32, R = 32 * WAVES, threads = 64 * WAVES;
     static constexpr int blocks = TN / 32, groups = TN / 16, steps = D / 16, operands = Columns<D>::operands;
     static constexpr int k_pitch = 2 * D + 16, v_pitch = 2 * TN + 16; // bytes
     static constexpr int k_bytes = TN * k_pitch, v_bytes = 32 * operands * v_pitch;
-    static constexpr int buffer = k_bytes + v_bytes + groups * 16; // and per 16 tokens: factor, addend, 1 / scale of V
+    static constexpr int buffer = k_bytes + v_bytes + groups * 16; // and per 16 tokens: factor, addend, 1 / what V's scale has in the exponent
     static constexpr int k_units = TN * D / 16, v_units = TN * D / 16;
     static constexpr int per_thread = (k_units + threads - 1) / threads;
     static constexpr int lds = 2 * buffer + D * 4;
@@ -146,6 +146,8 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     uint32_t vw[N][4];              // 4 columns of 4 tokens
     float ks = 0.f, vs = 1.f, v_scale[N];
     int k_token[N], v_token[N], k_at[N], v_at[N]; // this lane's: tokens of a tile, offsets in a token
+    const uint8_t *const k_head = p.k + h * p.k_head, *const v_head = p.v + h * p.v_head;
+    const auto page = [&](const uint8_t *head, int id, int64_t stride) __attribute__((always_inline)) { return head + (uint64_t)(uint32_t)id * (uint32_t)stride; };
 #pragma unroll
     for (int u = 0; u < N; ++u) { // (lanes beyond the last unit load that one again and store nothing)
         const int unit = K::k_units % K::threads != 0 && tid + u * K::threads >= K::k_units ? K::k_units - 1 : tid + u * K::threads;
@@ -157,7 +159,8 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     // Nothing here waits for a load: entries are looked at when the loads of their tile are issued, a tile later, and what is not there
     // is read from the first page and dropped when it is stored.
     const auto entry = [&](int t) __attribute__((always_inline)) { return table[(t < s.seen ? t : s.seen - 1) >> p.page_log]; };
-    const auto valid = [&](int t, int id) __attribute__((always_inline)) { return t < s.seen && id >= 0 && id < p.pages; };
+    const auto valid = [&](int t, int id) __attribute__((always_inline)) { return t < s.seen && (uint32_t)id < (uint32_t)p.pages; };
+    const auto scale = [&](const float *scales, int id, int64_t stride) __attribute__((always_inline)) { return scales + h + (uint64_t)(uint32_t)id * (uint32_t)stride; };
     const auto look_up = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -171,19 +174,19 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         for (int u = 0; u < N; ++u) {
             k_there[u] = valid(t0 + k_token[u], k_id[u]);
             const int ki = k_there[u] ? k_id[u] : 0;
-            kw[u] = *(const u32x4 *)(p.k + ki * p.k_page + h * p.k_head + ((t0 + k_token[u]) & in_page) * D + k_at[u]);
+            kw[u] = *(const u32x4 *)(page(k_head, ki, p.k_page) + (((t0 + k_token[u]) & in_page) * D + k_at[u]));
             v_there[u] = valid(t0 + v_token[u], v_id[u]);
             const int vi = v_there[u] ? v_id[u] : 0;
-            const uint8_t *v = p.v + vi * p.v_page + h * p.v_head + ((t0 + v_token[u]) & in_page) * D + v_at[u];
+            const uint8_t *v = page(v_head, vi, p.v_page) + (((t0 + v_token[u]) & in_page) * D + v_at[u]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) vw[u][r] = *(const uint32_t *)(v + r * D);
-            if (!K::f16) v_scale[u] = p.v_scale[vi * p.vs_page + h];
+            if (!K::f16) v_scale[u] = *scale(p.v_scale, vi, p.vs_page);
         }
         if (tid < K::groups) {
             there = valid(t0 + 16 * tid, g_id);
             const int id = there ? g_id : 0;
-            ks = p.k_scale[id * p.ks_page + h];
-            vs = p.v_scale[id * p.vs_page + h];
+            ks = *scale(p.k_scale, id, p.ks_page);
+            vs = *scale(p.v_scale, id, p.vs_page);
         }
     };
     const auto store = [&](uint8_t *buf, int t0) __attribute__((always_inline)) {
@@ -191,11 +194,19 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             if (K::k_units % K::threads != 0 && tid + u * K::threads >= K::k_units) continue;
+            if (__any(!k_there[u] || !v_there[u])) {
+                if (!k_there[u]) kw[u] = u32x4{0, 0, 0, 0};
+                if (!v_there[u]) {
+                    v_scale[u] = 1.f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) vw[u][r] = 0;
+                }
+            }
             {
                 u32x4 lo, hi;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t x = k_there[u] ? kw[u][e] : 0, y = k_there[u] ? kw[u][2 + e] : 0;
+                    const uint32_t x = kw[u][e], y = kw[u][2 + e];
                     lo[2 * e] = Wide<T>::template two<false>(x, 1.f);
                     lo[2 * e + 1] = Wide<T>::template two<true>(x, 1.f);
                     hi[2 * e] = Wide<T>::template two<false>(y, 1.f);
@@ -205,8 +216,6 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
                 *(u32x4 *)(buf + k_token[u] * K::k_pitch + 2 * k_at[u] + 16) = hi;
             }
             const int token = v_token[u], c = v_at[u] / 4;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) vw[u][r] = v_there[u] ? vw[u][r] : 0;
             if (hides) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -233,7 +242,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // tokens 4t of 16 stand at 8 (t % 2) + 4 (t / 2), the order of S^T's result
             const int t = token >> 2, place = (token & ~15) + 8 * (t & 1) + 4 * ((t >> 1) & 1);
             uint8_t *const to = buf + K::k_bytes + 2 * place;
-            const float sv = K::f16 || !v_there[u] ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
+            const float sv = K::f16 ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
@@ -242,7 +251,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // what of V's scale is not in V goes to the exponent: all of it (fp16), or what it is beyond its power of two
             const float v = !there ? 1.f : K::f16 ? fminf(fmaxf(vs, 0x1p-60f), 0x1p60f) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
             // (a factor of zero would make NaN of the -inf that hides a token)
-            const f32x4 x = {!there ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, there ? __builtin_amdgcn_logf(v) : -INFINITY, 1.0f / v, 0.f};
+            const f32x4 x = {!there ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, there ? __builtin_amdgcn_logf(v) : -INFINITY, __builtin_amdgcn_rcpf(v), 0.f};
             *(f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * tid) = x;
         }
     };
@@ -258,12 +267,21 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         f32x16 sc[K::blocks];
         const uint8_t *kp = buf + i * K::k_pitch + 16 * g;
 #pragma unroll
-        for (int j = 0; j < K::blocks; ++j) {
+        for (int j = 0; j < K::blocks; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sc[j][r] = 0.f;
 #pragma unroll
-            for (int c = 0; c < K::steps; ++c) sc[j] = Wide<T>::run(*(const v8 *)(kp + 32 * j * K::k_pitch + 32 * c), q[c], sc[j]);
+        for (int c = 0; c < K::steps; ++c)
+#pragma unroll
+            for (int j = 0; j < K::blocks; ++j) sc[j] = Wide<T>::run(*(const v8 *)(kp + 32 * j * K::k_pitch + 32 * c), q[c], sc[j]);
+        // six operands on their way before the first product, then one more behind each
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int z = 0; z < K::blocks * K::steps - 6; ++z) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
         f32x4 par[K::groups];
 #pragma unroll
         for (int k = 0; k < K::groups; ++k) par[k] = *(const f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * k);
@@ -294,22 +312,20 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
                 for (int r = 0; r < 16; ++r) o[c][r] *= by;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        v8 pw[K::groups];
+        const uint8_t *vp = buf + K::k_bytes + i * K::v_pitch + 16 * g;
 #pragma unroll
         for (int k = 0; k < K::groups; ++k) {
+            v8 pw;
             const float add = par[k][1] - ref;
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][8 * (k & 1) + r], par[k][0], add));
                 l = __builtin_fmaf(w, par[k][2], l);
-                pw[k][r] = (T)w;
+                pw[r] = (T)w;
             }
+#pragma unroll
+            for (int c = 0; c < K::operands; ++c) o[c] = Wide<T>::run(*(const v8 *)(vp + 32 * c * K::v_pitch + 32 * k), pw, o[c]);
         }
-        const uint8_t *vp = buf + K::k_bytes + i * K::v_pitch + 16 * g;
-#pragma unroll
-        for (int c = 0; c < K::operands; ++c)
-#pragma unroll
-            for (int k = 0; k < K::groups; ++k) o[c] = Wide<T>::run(*(const v8 *)(vp + 32 * c * K::v_pitch + 32 * k), pw[k], o[c]);
     };
 
     if (from < end) {
@@ -323,13 +339,18 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         lds_barrier();
         int turn = 0;
         for (int t0 = from; t0 < end; t0 += TN) {
+            const auto stage = [&]() __attribute__((always_inline)) {
+                if (t0 + TN < end) {
+                    store(lds + (turn ^ 1) * K::buffer, t0 + TN);
+                    load(t0 + 2 * TN);
+                    look_up(t0 + 3 * TN);
+                }
+            };
+            const bool early = wave & (WAVES / 2);
+            if (early) stage();
             if (t0 < wave_last) compute(lds + turn * K::buffer, t0);
+            if (!early) stage();
             turn ^= 1;
-            if (t0 + TN < end) {
-                store(lds + turn * K::buffer, t0 + TN);
-                load(t0 + 2 * TN);
-                look_up(t0 + 3 * TN);
-            }
             lds_barrier();
         }
     } else {

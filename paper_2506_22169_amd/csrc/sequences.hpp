@@ -144,7 +144,7 @@ inline int check_cache(const mcf_kv_cache &c) {
     for (const int64_t *s : {c.k_stride, c.v_stride}) {
         const int64_t sp = c.pages > 1 ? s[0] : 0, sh = c.heads > 1 ? s[1] : 0;
         if (sp % 16 != 0 || sh % 16 != 0) return MCF_EALIGN;
-        if (sp < 0 || sh < 0 || sp >= (1ll << 60) / c.pages || sh >= (1ll << 60) / c.heads) return MCF_EUNSUPPORTED;
+        if (sp < 0 || sh < 0 || sp >= 1ll << 32 || sh >= (1ll << 60) / c.heads) return MCF_EUNSUPPORTED; // (page numbers times 32 bits)
         // pages and heads may lie in either order, but not on top of one another
         const bool heads_inside = sh <= sp || c.pages == 1;
         const int64_t in = heads_inside ? sh : sp, n_in = heads_inside ? c.heads : c.pages, outer = heads_inside ? sp : sh, n_out = heads_inside ? c.pages : c.heads;
