@@ -68,6 +68,12 @@ template <int R> __device__ __forceinline__ uint32_t tiles_of(const Params &p, c
     return (uint32_t)(((int64_t)s.rows * p.group + R - 1) / R);
 }
 
+// What a row sees: tokens 0 .. limit - 1.
+__device__ __forceinline__ int limit_of(const Params &p, const Sequence &s, int token) { // token: of the sequence's rows
+    const int n = s.length - s.rows + token + 1;
+    return !p.causal || n > s.seen ? s.seen : n < 0 ? 0 : n;
+}
+
 // ---- few rows: pieces of the line ----
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
 // Piece j of the line: its first unit and the one behind it, and where the first lies: the sequence and the units before it there.
@@ -136,10 +142,48 @@ template <int R> __device__ __forceinline__ int chunk_of(const Params &p) {
 }
 __device__ __forceinline__ uint32_t chunks_of(const Sequence &s, int chunk) { return s.seen > chunk ? (uint32_t)((s.seen - 1) / chunk) + 1 : 1u; }
 
-// What a row sees: tokens 0 .. limit - 1.
-__device__ __forceinline__ int limit_of(const Params &p, const Sequence &s, int token) { // token: of the sequence's rows
-    const int n = s.length - s.rows + token + 1;
-    return !p.causal || n > s.seen ? s.seen : n < 0 ? 0 : n;
+// Tiles of a sequence whose last row sees more than x tokens (x < 0: all of them); these are its last.
+template <int R> __device__ __forceinline__ uint32_t tiles_beyond(const Params &p, const Sequence &s, int x) {
+    const uint32_t tiles = tiles_of<R>(p, s);
+    if (x < 0) return tiles;
+    if (x >= s.seen) return 0;
+    if (!p.causal) return tiles;
+    const int y = x - (s.length - s.rows); // token y of its rows sees y + 1 + length - rows
+    if (y < 0) return tiles;
+    const uint32_t first = (uint32_t)((int64_t)y * p.group / R);
+    return y < s.rows && first < tiles ? tiles - first : 0;
+}
+
+// Tile number `slot` of all tiles (of up to 64 sequences) by what they see, the most first, in 64 classes: a unit's last block is short then.
+template <int R> __device__ __forceinline__ bool locate_longest(const Params &p, uint32_t slot, int *b, uint32_t *tile, Sequence *s) {
+    const int lane = threadIdx.x & 63;
+    Sequence q = {0, 0, 0, 0};
+    if (lane < p.seq.batch) q = sequence(p.seq, lane);
+    int most = q.seen;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) { const int x = __shfl_xor(most, d); most = x > most ? x : most; }
+    const auto of = [&](const Sequence &x, int i) __attribute__((always_inline)) -> Sequence {
+        return {__builtin_amdgcn_readlane(x.first, i), __builtin_amdgcn_readlane(x.rows, i), __builtin_amdgcn_readlane(x.length, i), __builtin_amdgcn_readlane(x.seen, i)};
+    };
+    const auto border = [&](int i) __attribute__((always_inline)) { return i == 63 ? -1 : (int)((int64_t)most * (63 - i) >> 6); };
+    uint32_t upto = 0; // tiles beyond this lane's border
+    for (int i = 0; i < p.seq.batch; ++i) upto += tiles_beyond<R>(p, of(q, i), border(lane));
+    const uint64_t hit = __ballot(upto > slot);
+    if (!hit) return false;
+    const int c = __builtin_ctzll(hit);
+    const uint32_t before = c > 0 ? tiles_beyond<R>(p, q, border(c - 1)) : 0, n = tiles_beyond<R>(p, q, border(c)) - before;
+    slot -= c > 0 ? __builtin_amdgcn_readlane(upto, c - 1) : 0;
+    uint32_t sum = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t x = __shfl_up(sum, d);
+        if (lane >= d) sum += x;
+    }
+    const int i = __builtin_ctzll(__ballot(slot - (sum - n) < n));
+    *s = of(q, i);
+    *b = i;
+    *tile = tiles_of<R>(p, *s) - 1 - __builtin_amdgcn_readlane(before, i) - (slot - (__builtin_amdgcn_readlane(sum, i) - __builtin_amdgcn_readlane(n, i)));
+    return true;
 }
 
 int launch_rows_f16(const Params &p, int size, int row_blocks, unsigned blocks, void *stream);  // returns hipError_t as int

@@ -78,7 +78,7 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 template <typename T, int D, int WAVES> struct Tiles {
     typedef typename Wide<T>::v8 v8;
     static constexpr bool f16 = std::is_same<T, _Float16>::value;
-    static constexpr int TN = D <= 96 ? 128 : D <= 128 ? 64 : 32, R = 32 * WAVES, threads = 64 * WAVES;
+    static constexpr int TN = D <= 96 && WAVES == 8 ? 128 : D <= 128 ? 64 : 32, R = 32 * WAVES, threads = 64 * WAVES;
     static constexpr int blocks = TN / 32, groups = TN / 16, steps = D / 16, operands = Columns<D>::operands;
     static constexpr int k_pitch = 2 * D + 16, v_pitch = 2 * TN + 16; // bytes
     static constexpr int k_bytes = TN * k_pitch, v_bytes = 32 * operands * v_pitch;
@@ -98,16 +98,24 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     const int h = (int)(blockIdx.x - slot * p.heads);
     const int chunk = __builtin_amdgcn_readfirstlane(chunk_of<R>(p));
     int b;
-    uint32_t rest;
+    uint32_t tile, ch = 0, chunks = 1;
     Sequence s;
-    if (!locate_sequence(p.seq, slot, [&](const Sequence &q) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, q) * chunks_of(q, chunk); }, &b, &rest, &s)) {
-        if (p.split && threadIdx.x == 0) p.splits[blockIdx.x].parts = 0;
-        return;
+    if (!p.split && p.seq.batch <= 64) {
+        if (!locate_longest<R>(p, slot, &b, &tile, &s)) return;
+    } else {
+        uint32_t rest;
+        if (!locate_sequence(p.seq, slot, [&](const Sequence &q) __attribute__((always_inline)) -> uint32_t { return tiles_of<R>(p, q) * chunks_of(q, chunk); }, &b, &rest, &s)) {
+            if (p.split && threadIdx.x == 0) p.splits[blockIdx.x].parts = 0;
+            return;
+        }
+        rest = __builtin_amdgcn_readfirstlane(rest);
+        chunks = chunks_of(s, chunk);
+        tile = rest / chunks;
+        ch = rest - tile * chunks;
+        tile = tiles_of<R>(p, s) - 1 - tile; // the last rows, which see most, first
     }
     b = __builtin_amdgcn_readfirstlane(b);
-    rest = __builtin_amdgcn_readfirstlane(rest);
-    const uint32_t chunks = chunks_of(s, chunk), at = rest / chunks, ch = rest - at * chunks;
-    const uint32_t tile = tiles_of<R>(p, s) - 1 - at; // the last rows, which see most, first
+    tile = __builtin_amdgcn_readfirstlane(tile);
     const int rows = s.rows * p.group - (int)tile * R < R ? s.rows * p.group - (int)tile * R : R;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i = lane & 31, g = lane >> 5;
     const auto token_of = [&](int r) __attribute__((always_inline)) { return (int)quotient(tile * R + r, p.group_magic, p.group_shift); };

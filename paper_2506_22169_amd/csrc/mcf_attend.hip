@@ -106,7 +106,8 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     int64_t slots = resident_blocks(R, m.size) / m.heads;
     bool split = may_split;
     if (R > 64) {
-        split = split && slots > tiles;
+        // two chunks a tile at least, of tokens that are worth the parts' way through memory (256 rows of 128: 10 us) and a second kernel
+        split = split && slots >= 2 * tiles && c->seq.table_width * m.page_size > 1024;
         if (!split) slots = tiles;
     } else {
         // no more pieces than the longest sequences that the table holds would give; the line in 31 bits
