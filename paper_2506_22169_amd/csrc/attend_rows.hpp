@@ -10,12 +10,12 @@
 //  - V's operand wants 8 tokens of one column in a lane, memory has columns side by side: a lane reads size / 16 neighbouring
 //    columns of each of its 8 tokens (whole rows over the 16 lanes) and turns bytes in registers (v_perm); column i of
 //    product j is then column (size / 16) i + j of V, which leaves a lane with neighbouring columns of the result.
-//  - e4m3 -> 16 bit is exact; the scale of K multiplies the scores, that of V the weights, both in fp32.
+//  - e4m3 -> 16 bit is exact; the scale of K multiplies the scores in fp32.
 //
-// Weights.  bf16: p = 2^(s - m), rounded to bf16 after the factor of V's scale (bf16 has fp32's range).  fp16: V's scale is an
-// exponent like the score's, w = 2^(s + log2 scale - m) <= 2^8 with its own running reference, and the sum of the softmax adds
-// w / scale: the largest weight stands near 1 whatever the scales, where fp16 has all its bits.  Each weight is rounded once.
-// The reference m moves only when a score outgrows it by 2^8.
+// Weights.  V's scale is an exponent like the score's: w = 2^(s + log2 scale - m), m the running reference of these sums, and the
+// sum of the softmax adds w / scale; the largest weight stands near 1 whatever the scales, where fp16 has all its bits.  For bf16
+// (with fp32's range) the power of two of the scale is in V instead, where the widening instruction takes it, and only the rest of it in
+// the exponent.  Each weight is rounded once.  The reference moves only when a score outgrows it by 2^8.  Scales of K are not negative.
 //
 // Rows see prefixes of the tokens.  What no row of the tile sees is read as zero; where only some see a token whose value is NaN
 // (0 NaN would be NaN for the others), its column's NaN are counted by a matrix product with who sees them.
@@ -40,19 +40,27 @@ template <typename T> struct Mma;
 template <> struct Mma<_Float16> {
     typedef f16x8 v8;
     static __device__ __forceinline__ f32x4 run(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ uint32_t lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false)); }
-    static __device__ __forceinline__ uint32_t hi(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true)); }
+    static __device__ __forceinline__ uint32_t lo(uint32_t x, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, s, false)); }
+    static __device__ __forceinline__ uint32_t hi(uint32_t x, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, s, true)); }
 };
 template <> struct Mma<__bf16> {
     typedef bf16x8 v8;
     static __device__ __forceinline__ f32x4 run(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ uint32_t lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false)); }
-    static __device__ __forceinline__ uint32_t hi(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true)); }
+    static __device__ __forceinline__ uint32_t lo(uint32_t x, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, false)); }
+    static __device__ __forceinline__ uint32_t hi(uint32_t x, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, true)); }
 };
-// Eight e4m3 values (in the order of their bytes) as an operand.
-template <typename T> __device__ __forceinline__ typename Mma<T>::v8 widen(uint32_t a, uint32_t b) {
-    const u32x4 w = {Mma<T>::lo(a), Mma<T>::hi(a), Mma<T>::lo(b), Mma<T>::hi(b)};
+// Eight e4m3 values (in the order of their bytes) as an operand, four times the power of two of sa, four that of sb.
+template <typename T> __device__ __forceinline__ typename Mma<T>::v8 widen(uint32_t a, uint32_t b, float sa = 1.f, float sb = 1.f) {
+    const u32x4 w = {Mma<T>::lo(a, sa), Mma<T>::hi(a, sa), Mma<T>::lo(b, sb), Mma<T>::hi(b, sb)};
     return __builtin_bit_cast(typename Mma<T>::v8, w);
+}
+
+// The largest over the four lanes that hold one row.
+__device__ __forceinline__ float over_groups(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // Byte i of four words as one word, for i = 0 .. 3.
@@ -147,7 +155,7 @@ template <typename T, int D, int NB> struct Rows {
     }
 
     // f(first operand, j) for every product j: 8 tokens of column Cols::of(lane, j)
-    template <typename F> static __device__ __forceinline__ void each_product(const uint32_t v[8][C::regs], F f) {
+    template <typename F> static __device__ __forceinline__ void each_product(const uint32_t v[8][C::regs], float s0, float s1, F f) {
 #pragma unroll
         for (int w = 0; w < C::regs; ++w) {
             uint32_t lo[4], hi[4];
@@ -155,7 +163,7 @@ template <typename T, int D, int NB> struct Rows {
             turn_bytes(v[4][w], v[5][w], v[6][w], v[7][w], hi);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (4 * w + e < C::tiles) f(widen<T>(lo[e], hi[e]), 4 * w + e);
+                if (4 * w + e < C::tiles) f(widen<T>(lo[e], hi[e], s0, s1), 4 * w + e);
         }
     }
 
@@ -164,20 +172,30 @@ template <typename T, int D, int NB> struct Rows {
         f32x4 o[NB][C::tiles];
         float m[NB], l[NB]; // reference (-inf: nothing seen) and this lane's part of the sum
         int limit[NB];
+        float c; // |scale| log2(e): a negative scale turns the queries' signs
     };
 
     // 32 tokens from t; HIDE: some of them some row does not see (none sees those from `end` on, all see those below `all`)
     template <bool HIDE> static __device__ __forceinline__ void step(const Params &p, Step<D> &x, int t, int end, int all, State &st) {
         const int lane = threadIdx.x & 63, g = lane >> 4;
         v8 pw[NB];
-        float sv[2], lsv[2];
+        // factor and addend of the scores, and what V's scale put into the exponent: all of it (fp16), or what is beyond its power of two
+        float f[2], add[2], inv[2], sv[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            sv[j] = x.sv[j];
-            if constexpr (f16) {
-                sv[j] = fminf(fmaxf(sv[j], 0x1p-60f), 0x1p60f);
-                lsv[j] = __builtin_amdgcn_logf(sv[j]);
-                sv[j] = 1.0f / sv[j];
+            const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(f16 ? fminf(fmaxf(x.sv[j], 0x1p-60f), 0x1p60f) : x.sv[j]));
+            sv[j] = f16 ? 1.f : __uint_as_float(bits);
+            f[j] = st.c * x.sk[j];
+            if (f[j] < 0x1p-126f) f[j] = 0x1p-126f; // (zero would make NaN of the -inf that hides a token)
+            add[j] = x.hide[j];
+            inv[j] = 1.f;
+            if ((bits & 0x7fffff) != 0) { // no power of two
+                const float v = __uint_as_float(f16 ? bits : (bits & 0x7fffff) | 0x3f800000);
+                add[j] += __builtin_amdgcn_logf(v);
+                inv[j] = __builtin_amdgcn_rcpf(v);
+            } else if (f16) {
+                add[j] += (float)((int)(bits >> 23) - 127);
+                inv[j] = __uint_as_float((254 - (bits >> 23)) << 23);
             }
         }
         f32x4 sc[NB][2];
@@ -195,18 +213,16 @@ template <typename T, int D, int NB> struct Rows {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             f32x4 (&s)[2] = sc[n];
+            float most = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float f = p.c * x.sk[j], add = f16 ? lsv[j] + x.hide[j] : x.hide[j];
+                if (HIDE) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[j][r] = __builtin_fmaf(s[j][r], f, add);
-                    if (HIDE && t + 16 * j + 4 * g + r >= st.limit[n]) s[j][r] = -INFINITY;
+                    for (int r = 0; r < 4; ++r) s[j][r] = t + 16 * j + 4 * g + r >= st.limit[n] ? -INFINITY : s[j][r];
                 }
+                most = fmaxf(most, __builtin_fmaf(fmaxf(fmaxf(s[j][0], s[j][1]), fmaxf(s[j][2], s[j][3])), f[j], add[j]));
             }
-            float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
+            most = over_groups(most);
             if (__any(most > st.m[n] + 8.f)) {
                 const float m = fmaxf(most, st.m[n]);
                 const float by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
@@ -220,9 +236,9 @@ template <typename T, int D, int NB> struct Rows {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float w = __builtin_amdgcn_exp2f(s[j][r] - m);
-                    st.l[n] = f16 ? __builtin_fmaf(w, sv[j], st.l[n]) : st.l[n] + w;
-                    pw[n][4 * j + r] = (T)(f16 ? w : w * sv[j]);
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], f[j], add[j] - m));
+                    st.l[n] = __builtin_fmaf(w, inv[j], st.l[n]);
+                    pw[n][4 * j + r] = (T)w;
                 }
         }
         if constexpr (HIDE) {
@@ -241,7 +257,7 @@ template <typename T, int D, int NB> struct Rows {
                 if (__any(nan)) count_nans(x, t, st);
             }
         }
-        each_product(x.v, [&](const v8 &a, int j) __attribute__((always_inline)) {
+        each_product(x.v, sv[0], sv[1], [&](const v8 &a, int j) __attribute__((always_inline)) {
 #pragma unroll
             for (int n = 0; n < NB; ++n) st.o[n][j] = Mma<T>::run(a, pw[n], st.o[n][j]);
         });
@@ -264,7 +280,7 @@ template <typename T, int D, int NB> struct Rows {
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sees[b][e] = t + 16 * (e >> 2) + 4 * g + (e & 3) < st.limit[b] ? (T)1.f : (T)0.f;
-        each_product(ones, [&](const v8 &a, int j) __attribute__((always_inline)) {
+        each_product(ones, 1.f, 1.f, [&](const v8 &a, int j) __attribute__((always_inline)) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const f32x4 n = Mma<T>::run(a, sees[b], f32x4{0.f, 0.f, 0.f, 0.f});
@@ -287,34 +303,43 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
     const int last = limit_of(p, s, token_of(rows < R ? rows - 1 : R - 1)), all = limit_of(p, s, token_of(0));
     const int end = to < last ? to : last;
 
+    // The first entries of the table, the queries and the first keys and values, each asked for before anything waits.
+    const int32_t *const table = p.seq.table + b * p.seq.table_stride;
+    int t = (from < end ? from : end) + 32 * wave, id[2];
+    const int plain = all < end ? all : end; // every row sees the tokens below
+    if (t < end) K::look_up(p, table, t, s.seen, id);
     typename K::State st;
+    u32x4 q[NB][K::steps];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-        const int r = 16 * n + i;
-        const bool real = r < rows;
-        const int t = token_of(real ? r : 0), head = tile * R + (real ? r : 0) - t * p.group;
-        st.limit[n] = real ? limit_of(p, s, t) : s.seen; // (rows that pad the tile hide nothing)
+        const int r = 16 * n + i < rows ? 16 * n + i : 0, tk = token_of(r), head = tile * R + r - tk * p.group;
+        st.limit[n] = 16 * n + i < rows ? limit_of(p, s, tk) : s.seen; // (rows that pad the tile hide nothing)
+        const T *at = (const T *)p.q + (int64_t)(s.first + tk) * p.qt + (int64_t)(h * p.group + head) * p.qh;
+#pragma unroll
+        for (int c = 0; c < K::steps; ++c) q[n][c] = *(const u32x4 *)(at + (D % 32 == 0 || K::part(c, g) < D ? K::part(c, g) : 0));
+    }
+    Step<D> x;
+    const bool many = t + 32 <= plain;
+    if (many) {
+        K::load(p, h, t, s.seen, id, x);
+        K::look_up(p, table, t + kUnit, s.seen, id);
+    }
+    st.c = fabsf(p.c);
+    const uint32_t sign = p.c < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
         st.m[n] = -INFINITY;
         st.l[n] = 0.f;
-        const T *q = (const T *)p.q + (int64_t)(s.first + t) * p.qt + (int64_t)(h * p.group + head) * p.qh;
 #pragma unroll
         for (int c = 0; c < K::steps; ++c) {
-            const bool in = real && (D % 32 == 0 || K::part(c, g) < D);
-            const u32x4 w = *(const u32x4 *)(q + (in ? K::part(c, g) : 0));
-            st.q[n][c] = __builtin_bit_cast(typename K::v8, in ? w : u32x4{0, 0, 0, 0});
+            const bool in = 16 * n + i < rows && (D % 32 == 0 || K::part(c, g) < D);
+            st.q[n][c] = __builtin_bit_cast(typename K::v8, in ? q[n][c] ^ sign : u32x4{0, 0, 0, 0});
         }
 #pragma unroll
         for (int c = 0; c < C::tiles; ++c) st.o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int32_t *const table = p.seq.table + b * p.seq.table_stride;
-    int t = (from < end ? from : end) + 32 * wave;
-    const int plain = all < end ? all : end; // every row sees the tokens below
-    int id[2];
-    if (t < end) K::look_up(p, table, t, s.seen, id);
-    if (t + 32 <= plain) {
-        Step<D> x, next;
-        K::load(p, h, t, s.seen, id, x);
-        K::look_up(p, table, t + kUnit, s.seen, id);
+    if (many) {
+        Step<D> next;
         for (;;) {
             const int u = t + kUnit;
             const bool more = u + 32 <= plain;
@@ -329,7 +354,6 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
         }
     }
     for (; t < end; t += kUnit) {
-        Step<D> x;
         K::load(p, h, t, s.seen, id, x);
         K::look_up(p, table, t + kUnit, s.seen, id);
         K::template step<true>(p, x, t, end, all, st);
@@ -431,7 +455,10 @@ template <typename T> int launch_rows(const Params &p, int size, int row_blocks,
         constexpr int D = decltype(d)::value;
         if (row_blocks == 1) hipLaunchKernelGGL((rows_kernel<T, D, 1>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
         else if (row_blocks == 2) hipLaunchKernelGGL((rows_kernel<T, D, 2>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
-        else if constexpr (D <= 128) hipLaunchKernelGGL((rows_kernel<T, D, 4>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+        else if constexpr (D <= 128) {
+            if (row_blocks == 3) hipLaunchKernelGGL((rows_kernel<T, D, 3>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+            else if constexpr (D <= 64) hipLaunchKernelGGL((rows_kernel<T, D, 4>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+        }
     };
     switch (size) {
     case 64: go(std::integral_constant<int, 64>()); break;

@@ -13,8 +13,7 @@
 //    neighbouring columns of the result.
 //  - Padding of 16 bytes a row puts the rows of both on different banks.
 //
-// Weights and what rows do not see: as attend_rows.hpp does it for fp16, but for bf16 the power of two of V's scale is in V and only what it is
-// beyond that in the exponent.  Scales of K are not negative.  A NaN in V that only some
+// Weights and what rows do not see: as in attend_rows.hpp.  A NaN in V that only some
 // rows of the tile see is taken out and its first token noted for its column; rows that see that token get NaN.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -300,7 +299,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sc[j][r] = 32 * j + 8 * (r >> 2) + (r & 3) < room ? sc[j][r] : -INFINITY;
         }
-        // the largest of each 16 tokens, whose factor is one and not negative, then of all of them
+        // the largest of each 16 tokens, which have one factor, then of all of them
         float most = -INFINITY;
 #pragma unroll
         for (int k = 0; k < K::groups; ++k) {

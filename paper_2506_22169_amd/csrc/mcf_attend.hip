@@ -67,7 +67,7 @@ template <typename T> __global__ __launch_bounds__(256) void join_kernel(const P
 
 struct Plan {
     Params p;
-    int tile_rows;          // 16, 32, 64: attend_rows.hpp; 128, 256: attend_tiles.hpp
+    int tile_rows;          // 16, 32, 48, 64: attend_rows.hpp; 128, 256: attend_tiles.hpp
     unsigned tiles, blocks; // an upper bound of the tiles; 0 blocks: nothing to do
     int64_t workspace;      // what a split call wants
     int64_t places;         // of parts there
@@ -99,9 +99,11 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     if (tokens == 0 || batch == 0 || c->q_heads == 0) return MCF_OK;
     const int64_t group = c->q_heads / m.heads;
     if (group > 1 << 16 || tokens * group >= (1ll << 31) - 65536) { set_last_error("too many rows for one call"); return MCF_EUNSUPPORTED; }
-    // the rows that a sequence brings in the mean decide the tile
+    // The rows that a sequence brings in the mean decide the tile.  Where both kernels could: 16 sequences of 16 tokens against 4000, 32 heads on 8
+    // (64 rows), take 43 us with the few rows' kernel and 48 with the other for heads of 64, 86 and 67 for heads of 128 (48 rows: 67 both;
+    // 5 tokens of 16 heads on 2 of 64 against 130000, 40 rows: 26 and 74).
     const int64_t rows = (tokens * group + batch - 1) / batch;
-    const int R = o->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 && m.size <= 128 ? 64 : rows <= 128 ? 128 : 256;
+    const int R = o->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 && m.size <= 128 ? 48 : rows <= 64 && m.size <= 64 ? 64 : rows <= 128 ? 128 : 256;
     const int64_t tiles = tokens * group / R + (batch < tokens ? batch : tokens);
     int64_t slots = resident_blocks(R, m.size) / m.heads;
     bool split = may_split;
