@@ -186,8 +186,8 @@ template <int R> __device__ __forceinline__ bool locate_longest(const Params &p,
     return true;
 }
 
-int launch_rows_f16(const Params &p, int size, int row_blocks, unsigned blocks, void *stream);  // returns hipError_t as int
-int launch_rows_bf16(const Params &p, int size, int row_blocks, unsigned blocks, void *stream);
+int launch_rows_f16(const Params &p, int size, int row_blocks, int waves, unsigned blocks, void *stream);  // returns hipError_t as int
+int launch_rows_bf16(const Params &p, int size, int row_blocks, int waves, unsigned blocks, void *stream);
 int launch_tiles_f16(const Params &p, int size, int waves, unsigned blocks, void *stream);
 int launch_tiles_bf16(const Params &p, int size, int waves, unsigned blocks, void *stream);
 

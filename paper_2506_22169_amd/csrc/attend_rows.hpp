@@ -293,10 +293,10 @@ template <typename T, int D, int NB> struct Rows {
 
 // The rows of one tile over its tokens from .. to - 1 (as far as it sees any); part < 0: all of them, the result is written; else what
 // they give goes to that place of the workspace.
-template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(const Params &p, const Sequence &s, int b, int h, uint32_t tile, int from, int to, int part_at) {
+template <typename T, int D, int NB, int WAVES> __device__ __forceinline__ void tile_part(const Params &p, const Sequence &s, int b, int h, uint32_t tile, int from, int to, int part_at) {
     typedef Rows<T, D, NB> K;
     typedef Cols<D> C;
-    constexpr int R = K::R, pitch = D + 4;
+    constexpr int R = K::R, pitch = D + 4, stride = 32 * WAVES;
     const int rows = s.rows * p.group - (int)tile * R; // of this tile, of R
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const auto token_of = [&](int r) __attribute__((always_inline)) { return (int)quotient(tile * R + r, p.group_magic, p.group_shift); };
@@ -322,7 +322,7 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
     const bool many = t + 32 <= plain;
     if (many) {
         K::load(p, h, t, s.seen, id, x);
-        K::look_up(p, table, t + kUnit, s.seen, id);
+        K::look_up(p, table, t + stride, s.seen, id);
     }
     st.c = fabsf(p.c);
     const uint32_t sign = p.c < 0.f ? 0x80008000u : 0u;
@@ -341,11 +341,11 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
     if (many) {
         Step<D> next;
         for (;;) {
-            const int u = t + kUnit;
+            const int u = t + stride;
             const bool more = u + 32 <= plain;
             if (more) {
                 K::load(p, h, u, s.seen, id, next);
-                K::look_up(p, table, u + kUnit, s.seen, id);
+                K::look_up(p, table, u + stride, s.seen, id);
             }
             K::template step<false>(p, x, t, end, all, st);
             t = u;
@@ -353,14 +353,14 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
             x = next;
         }
     }
-    for (; t < end; t += kUnit) {
+    for (; t < end; t += stride) {
         K::load(p, h, t, s.seen, id, x);
-        K::look_up(p, table, t + kUnit, s.seen, id);
+        K::look_up(p, table, t + stride, s.seen, id);
         K::template step<true>(p, x, t, end, all, st);
     }
 
-    // The four waves' parts: each scaled to the largest reference, then summed in the waves' order.
-    __shared__ float ref[4][R], sum[4][R];
+    // The waves' parts: each scaled to the largest reference, then summed in the waves' order (of eight, the last four to the first four before).
+    __shared__ float ref[WAVES][R], sum[WAVES][R];
     __shared__ float part[4][16 * pitch];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -368,28 +368,50 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
         st.l[n] += __shfl_xor(st.l[n], 32);
         if (g == 0) { ref[wave][16 * n + i] = st.m[n]; sum[wave][16 * n + i] = st.l[n]; }
     }
+    const auto top_of = [&](int r) __attribute__((always_inline)) {
+        float m = ref[0][r];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ref[w][r]);
+        return m;
+    };
     const int64_t place = ((int64_t)part_at * p.heads + h) * p.part_rows;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         __syncthreads();
-        const int r = 16 * n + i;
-        const float m = fmaxf(fmaxf(ref[0][r], ref[1][r]), fmaxf(ref[2][r], ref[3][r]));
-        const float by = st.m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[n] - m);
+        const float by = st.m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[n] - top_of(16 * n + i));
+        const auto put = [&](float *to) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < C::tiles; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[i * pitch + C::of(4 * g + e, c)] = st.o[n][c][e];
+        };
 #pragma unroll
         for (int c = 0; c < C::tiles; ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[wave][i * pitch + C::of(4 * g + e, c)] = st.m[n] == -INFINITY ? 0.f : st.o[n][c][e] * by;
+            for (int e = 0; e < 4; ++e) st.o[n][c][e] = st.m[n] == -INFINITY ? 0.f : st.o[n][c][e] * by;
+        if constexpr (WAVES == 8) {
+            if (wave >= 4) put(part[wave - 4]);
+            __syncthreads();
+            if (wave < 4) {
+#pragma unroll
+                for (int c = 0; c < C::tiles; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st.o[n][c][e] += part[wave][i * pitch + C::of(4 * g + e, c)];
+            }
+            __syncthreads();
+        }
+        if (wave < 4) put(part[wave]);
         __syncthreads();
-        for (int at = threadIdx.x * 4; at < 16 * D; at += 1024) {
+        for (int at = threadIdx.x * 4; at < 16 * D; at += 256 * WAVES) {
             const int q = at / D, d = at - q * D, row = 16 * n + q;
             if (row >= rows) continue;
             f32x4 o = *(const f32x4 *)&part[0][q * pitch + d];
 #pragma unroll
             for (int w = 1; w < 4; ++w) o += *(const f32x4 *)&part[w][q * pitch + d];
-            const float top = fmaxf(fmaxf(ref[0][row], ref[1][row]), fmaxf(ref[2][row], ref[3][row]));
+            const float top = top_of(row);
             float l = 0.f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) l += ref[w][row] == -INFINITY ? sum[w][row] : sum[w][row] * __builtin_amdgcn_exp2f(ref[w][row] - top); // (nothing seen: 0, or NaN by NaN scores)
+            for (int w = 0; w < WAVES; ++w) l += ref[w][row] == -INFINITY ? sum[w][row] : sum[w][row] * __builtin_amdgcn_exp2f(ref[w][row] - top); // (nothing seen: 0, or NaN by NaN scores)
             if (part_at >= 0) {
                 *(f32x4 *)(p.part + (place + row) * D + d) = o;
                 if (d == 0) { p.part_ml[2 * (place + row)] = top; p.part_ml[2 * (place + row) + 1] = l; }
@@ -407,7 +429,9 @@ template <typename T, int D, int NB> __device__ __forceinline__ void tile_part(c
     __syncthreads(); // (the shared parts are free again)
 }
 
-template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_simd(D, NB), waves_per_simd(D, NB)))) void rows_kernel(const Params p) {
+// Eight waves: calls that are not split (a tile a block), of sequences short enough.
+template <typename T, int D, int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVES == 8 ? 2 : waves_per_simd(D, NB), WAVES == 8 ? 2 : waves_per_simd(D, NB)))) void rows_kernel(const Params p) {
     typedef Rows<T, D, NB> K;
     constexpr int R = K::R;
     const uint32_t j = blockIdx.x / (uint32_t)p.heads;
@@ -431,7 +455,7 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribu
             const uint32_t tile = rest / units, x = rest - tile * units, n = units - x < end - at ? units - x : end - at;
             const int from = first_token(x), to = x + n == units ? 0x7fffffff : first_token(x + n);
             const bool whole = from == 0 && x + n == units;
-            if (from < to) tile_part<T, D, NB>(p, s, b, h, tile, from, to, whole ? -1 : (int)(2 * j + (from == 0)));
+            if (from < to) tile_part<T, D, NB, WAVES>(p, s, b, h, tile, from, to, whole ? -1 : (int)(2 * j + (from == 0)));
             if (from == 0 && to > 0) { // the first of one or more parts
                 const int rows = s.rows * p.group - (int)tile * R;
                 const Split first = {whole ? 0 : 1 + (int)((units - x - n + piece - 1) / piece), (int)(2 * j + 1), (int)(2 * j + 2), 2, s.first, (int)tile * R, rows < R ? rows : R, 0};
@@ -450,14 +474,17 @@ template <typename T, int D, int NB> __global__ __launch_bounds__(256) __attribu
     if (p.split && !p.by_tile && threadIdx.x == 0) p.splits[blockIdx.x] = split;
 }
 
-template <typename T> int launch_rows(const Params &p, int size, int row_blocks, unsigned blocks, void *stream) {
+template <typename T> int launch_rows(const Params &p, int size, int row_blocks, int waves, unsigned blocks, void *stream) {
     const auto go = [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (row_blocks == 1) hipLaunchKernelGGL((rows_kernel<T, D, 1>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
-        else if (row_blocks == 2) hipLaunchKernelGGL((rows_kernel<T, D, 2>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+        const dim3 grid(blocks), block(64 * waves);
+        hipStream_t st = (hipStream_t)stream;
+        if (waves == 8) hipLaunchKernelGGL((rows_kernel<T, D, 1, 8>), grid, block, 0, st, p);
+        else if (row_blocks == 1) hipLaunchKernelGGL((rows_kernel<T, D, 1, 4>), grid, block, 0, st, p);
+        else if (row_blocks == 2) hipLaunchKernelGGL((rows_kernel<T, D, 2, 4>), grid, block, 0, st, p);
         else if constexpr (D <= 128) {
-            if (row_blocks == 3) hipLaunchKernelGGL((rows_kernel<T, D, 3>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
-            else if constexpr (D <= 64) hipLaunchKernelGGL((rows_kernel<T, D, 4>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, p);
+            if (row_blocks == 3) hipLaunchKernelGGL((rows_kernel<T, D, 3, 4>), grid, block, 0, st, p);
+            else if constexpr (D <= 64) hipLaunchKernelGGL((rows_kernel<T, D, 4, 4>), grid, block, 0, st, p);
         }
     };
     switch (size) {

@@ -65,10 +65,15 @@ template <typename T> __global__ __launch_bounds__(256) void join_kernel(const P
     *(T4 *)((T *)p.out + (int64_t)(t.token + token) * p.ot + (int64_t)(h * p.group + head) * p.oh + d) = y;
 }
 
+// Keys of a sequence, in bytes, that one block of eight waves goes through: 500 tokens of 128 take 9.5 us (in pieces 11.9), 600 10.6 (12.9), 1000
+// 12.6 (11.8); 1000 of 64 10.6 (13.0).
+constexpr int64_t kShort = 96 << 10;
+
 struct Plan {
     Params p;
     int tile_rows;          // 16, 32, 48, 64: attend_rows.hpp; 128, 256: attend_tiles.hpp
     unsigned tiles, blocks; // an upper bound of the tiles; 0 blocks: nothing to do
+    int waves;              // of a block of few rows
     int64_t workspace;      // what a split call wants
     int64_t places;         // of parts there
 };
@@ -106,6 +111,7 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     const int R = o->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 && m.size <= 128 ? 48 : rows <= 64 && m.size <= 64 ? 64 : rows <= 128 ? 128 : 256;
     const int64_t tiles = tokens * group / R + (batch < tokens ? batch : tokens);
     int64_t slots = resident_blocks(R, m.size) / m.heads;
+    o->waves = 4;
     bool split = may_split;
     if (R > 64) {
         // two chunks a tile at least, of tokens that are worth the parts' way through memory (256 rows of 128: 10 us) and a second kernel
@@ -113,9 +119,12 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
         if (!split) slots = tiles;
     } else {
         // no more pieces than the longest sequences that the table holds would give; the line in 31 bits
-        const int64_t most = tiles * ((m.pages ? c->seq.table_width * m.page_size : 0) / kUnit + 2);
+        const int64_t reach = m.pages ? c->seq.table_width * m.page_size : 0;
+        const int64_t most = tiles * (reach / kUnit + 2);
         if (slots < 1) slots = 1;
         if (slots > (most + kLeast - 1) / kLeast) slots = (most + kLeast - 1) / kLeast;
+        // a tile a block of eight waves where the table ends early and there are units for all: one launch instead of two
+        if (R == 16 && reach * m.size <= kShort && tiles * m.heads <= kComputeUnits) { split = false; o->waves = 8; }
         split = split && most < 1ll << 31;
         if (!split) slots = tiles;
     }
@@ -194,7 +203,7 @@ extern "C" int mcf_cache_attention(const mcf_attention_call *c, void *workspace,
     const int size = (int)c->cache.size;
     const bool f16 = c->dtype == MCF_F16;
     int err;
-    if (l.tile_rows <= 64) err = (f16 ? attend::launch_rows_f16 : attend::launch_rows_bf16)(p, size, l.tile_rows / 16, l.blocks, stream);
+    if (l.tile_rows <= 64) err = (f16 ? attend::launch_rows_f16 : attend::launch_rows_bf16)(p, size, l.tile_rows / 16, l.waves, l.blocks, stream);
     else err = (f16 ? attend::launch_tiles_f16 : attend::launch_tiles_bf16)(p, size, l.tile_rows / 32, l.blocks, stream);
     if (err == hipSuccess && l.workspace > 0 && p.slots > 1) err = attend::launch_join(p, c->dtype, size, l.tile_rows, l.tiles, l.blocks, stream);
     if (err == hipSuccess) return MCF_OK;
