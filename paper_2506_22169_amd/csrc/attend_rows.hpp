@@ -460,7 +460,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
                 const int rows = s.rows * p.group - (int)tile * R;
                 const Split first = {whole ? 0 : 1 + (int)((units - x - n + piece - 1) / piece), (int)(2 * j + 1), (int)(2 * j + 2), 2, s.first, (int)tile * R, rows < R ? rows : R, 0};
                 if (!whole) split = first;
-                if (p.by_tile && threadIdx.x == 0) p.splits[(tiles_before + tile) * p.heads + h] = first;
+                // (starts that are not ascending can give more tiles than there is room for)
+                if (p.by_tile && threadIdx.x == 0 && tiles_before + tile < p.slots) p.splits[(tiles_before + tile) * p.heads + h] = first;
             }
             rest += n;
             at += n;

@@ -18,6 +18,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "attend.hpp"
@@ -411,8 +412,15 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
 
 template <typename T, int D, int WAVES> int launch_tile(const Params &p, unsigned blocks, void *stream) {
     typedef Tiles<T, D, WAVES> K;
-    static const hipError_t set = hipFuncSetAttribute((const void *)tiles_kernel<T, D, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, K::lds);
-    if (set != hipSuccess) return (int)set;
+    static std::atomic<uint64_t> set{0}; // devices that have been told
+    int device = 0;
+    hipError_t err = hipGetDevice(&device);
+    if (err != hipSuccess) return (int)err;
+    if (device >= 64 || !(set.load(std::memory_order_relaxed) >> device & 1)) {
+        err = hipFuncSetAttribute((const void *)tiles_kernel<T, D, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, K::lds);
+        if (err != hipSuccess) return (int)err;
+        if (device < 64) set.fetch_or(1ull << device, std::memory_order_relaxed);
+    }
     hipLaunchKernelGGL((tiles_kernel<T, D, WAVES>), dim3(blocks), dim3(K::threads), K::lds, (hipStream_t)stream, p);
     return (int)hipGetLastError();
 }

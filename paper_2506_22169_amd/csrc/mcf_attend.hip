@@ -19,7 +19,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
     const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once, block = blockIdx.x / groups;
     const int row0 = (int)(blockIdx.x - block * groups) * at_once, h = (int)(block % (uint32_t)p.heads);
-    if (p.by_tile && block >= (uint32_t)(*p.tiles * p.heads)) return;
+    if (p.by_tile && block / (uint32_t)p.heads >= (uint32_t)*p.tiles) return; // (tiles < slots: the grid ends within the room for them)
     const Split t = p.splits[block];
     if (t.parts == 0 || t.rows <= row0) return;
     const int quads = size / 4, slices = 256 / (quads * at_once);

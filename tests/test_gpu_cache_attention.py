@@ -189,6 +189,20 @@ def test_starts_of_no_order():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("tokens,heads,width", [(64, 16, 8), (64, 2, 8), (300, 16, 2), (64, 4, 100)])
+def test_starts_that_overlap(tokens, heads, width):
+    """Every second sequence claims all rows: many times the tiles that rows and sequences allow for."""
+    batch = 60
+    q = torch.randn(tokens, heads, 64).half().cuda()
+    c = mcf.kv_cache(8, 1, 16, 64)
+    table = torch.zeros(batch, width, dtype=torch.int32, device="cuda")
+    lengths = torch.full((batch,), 16 * width, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, tokens] * (batch // 2) + [0], dtype=torch.int32, device="cuda")
+    out = mcf.cache_attention(q, c, table, lengths, 0.1, starts)
+    torch.cuda.synchronize()
+    assert out.shape == q.shape
+
+
 def test_empty():
     c = mcf.kv_cache(2, 1, 16, 64)
     none = torch.zeros(0, dtype=torch.int32, device="cuda")
@@ -200,10 +214,10 @@ def test_empty():
         assert (mcf.cache_attention(q, cache, table, length, 1.0) == 0).all()
 
 
-def _long(dtype, new, n, pages_before=0):
+def _long(dtype, new, n, pages_before=0, size=128):
     """A long sequence and a 64-bit reference on the device."""
     gen = torch.Generator(device="cuda").manual_seed(37)
-    page, heads, size = 64, 1, 128
+    page, heads = 64, 1
     pages = pages_before + -(-n // page)
     c = mcf.kv_cache(pages, heads, page, size)
     used = c.k[pages_before:], c.v[pages_before:]
@@ -234,6 +248,59 @@ def _long(dtype, new, n, pages_before=0):
 @pytest.mark.parametrize("new", [1, 3, 150])
 def test_long(new, dtype):
     _long(dtype, new, 50001)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 7, 12, 16, 30, 60])
+@pytest.mark.parametrize("size", [64, 80, 96, 128, 192, 256])
+def test_parts(size, new, dtype):
+    """Tiles whose tokens are split over blocks, of every number of rows and every size."""
+    _long(dtype, new, 5003, size=size)
+
+
+@pytest.mark.parametrize("new,hq,heads", [(70, 2, 2), (1, 40, 2), (9, 4, 1)])
+def test_more_sequences_than_lanes(new, hq, heads):
+    """67 sequences, of one length that is long enough to be split and many short ones."""
+    gen = torch.Generator().manual_seed(39)
+    news = [new if i % 9 else 0 for i in range(67)]
+    lengths = [new + (3 * i) % 40 for i in range(66)] + [1500]
+    q, cache, host, table = _problem(gen, news, lengths, hq, heads, 64, 16, torch.bfloat16)
+    _check(q, cache, host, table, news, lengths, 16, 0.1, True)
+
+
+@pytest.mark.parametrize("new", [1, 3, 60])
+def test_captured_by_others(new):
+    """A stream that the HIP runtime captures for someone else has no workspace: the call is one kernel, and its replays equal the eager call."""
+    import ctypes
+    import re
+    hip = ctypes.CDLL(re.search(r"\S*/libamdhip64\.so\S*", open("/proc/self/maps").read()).group())
+    gen = torch.Generator().manual_seed(40)
+    q, cache, host, table = _problem(gen, [new], [2500], 4, 1, 64, 16, torch.float16)
+    starts = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    args = [q.cuda(), cache, table.int().cuda(), torch.tensor([2500]).int().cuda(), 0.1, starts]
+    out = mcf.cache_attention(*args)
+    want, bound = ref.attention(q, host[0], host[1], table, [new], [2500], 16, 0.1, True)
+    ref.check(out, want, bound, torch.float16)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    handle, graph, exe, n = ctypes.c_void_p(stream.cuda_stream), ctypes.c_void_p(), ctypes.c_void_p(), ctypes.c_size_t()
+    assert hip.hipStreamBeginCapture(handle, 1) == 0
+    try:
+        mcf.cache_attention(*args, out=out, stream=stream)
+        with pytest.raises(mcf.McfError) as refused:
+            mcf.norm_rotate_backward(args[0], None, args[0], q_weight=torch.ones(64, dtype=torch.float16, device="cuda"), stream=stream)
+    finally:
+        assert hip.hipStreamEndCapture(handle, ctypes.byref(graph)) == 0
+    assert refused.value.status == 2
+    assert hip.hipGraphGetNodes(graph, None, ctypes.byref(n)) == 0 and n.value == 1
+    assert hip.hipGraphInstantiate(ctypes.byref(exe), graph, None, None, ctypes.c_size_t(0)) == 0
+    for rep in range(3):
+        out.fill_(-3.0)
+        torch.cuda.synchronize()
+        assert hip.hipGraphLaunch(exe, handle) == 0
+        torch.cuda.synchronize()
+        ref.check(out, want, bound, torch.float16)
+    assert hip.hipGraphExecDestroy(exe) == 0 and hip.hipGraphDestroy(graph) == 0
 
 
 def test_beyond_32_bits():
