@@ -15,7 +15,8 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts of a tile, for `at_once` of its rows.  A row's lanes take four
-// elements of every slices-th part each; their sums are added in that order.
+// elements of every slices-th part each; their sums are added in that order.  Bound by latency: 4 to 6 us for the parts of 64 sequences' tiles
+// (20 MB), 8 for 5 x 8 rows of some 500 parts.
 template <typename T> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
     const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once, block = blockIdx.x / groups;
     const int row0 = (int)(blockIdx.x - block * groups) * at_once, h = (int)(block % (uint32_t)p.heads);
@@ -90,7 +91,7 @@ int plan(const mcf_attention_call *c, bool may_split, Plan *o) {
     if (c->dtype != MCF_F16 && c->dtype != MCF_BF16) return MCF_EUNSUPPORTED;
     const mcf_kv_cache &m = c->cache;
     int st = check_cache(m);
-    if (st == MCF_OK) st = check_sequences(c->seq, m.page_size);
+    if (st == MCF_OK) st = check_sequences(c->seq);
     if (st != MCF_OK) return st;
     if (!(c->scale - c->scale == 0.f)) return MCF_EINVAL; // NaN, infinity
     if (c->q_heads < 0 || (c->q_heads > 0 && (m.heads == 0 || c->q_heads % m.heads != 0))) {

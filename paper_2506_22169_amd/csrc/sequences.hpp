@@ -103,7 +103,7 @@ __device__ __forceinline__ int sequence_of_row(const Sequences &s, int t) {
     return lo < s.batch && s.starts[lo] <= t && t < s.starts[lo + 1] ? lo : -1;
 }
 
-inline int check_sequences(const mcf_sequences &s, int64_t page_size) {
+inline int check_sequences(const mcf_sequences &s) {
     if (s.batch < 0 || s.tokens < 0 || s.table_width < 0) return MCF_EINVAL;
     if (s.batch > (1 << 24) || s.tokens >= (1ll << 31) - 1024 || s.table_width >= 1ll << 31) return MCF_EUNSUPPORTED;
     if (s.batch > 0 && (!s.lengths || (s.table_width > 0 && !s.table))) return MCF_EINVAL;
@@ -111,7 +111,6 @@ inline int check_sequences(const mcf_sequences &s, int64_t page_size) {
     if (((uintptr_t)s.starts | (uintptr_t)s.lengths | (uintptr_t)s.table) % 4 != 0) return MCF_EALIGN;
     if (s.batch > 1 && s.table_stride < 0) return MCF_EINVAL;
     if (s.table_stride >= 1ll << 40) return MCF_EUNSUPPORTED;
-    (void)page_size;
     return MCF_OK;
 }
 

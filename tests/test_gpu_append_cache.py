@@ -161,6 +161,17 @@ def test_one_by_one_and_at_once(page, size):
             assert torch.equal(a[big], b[big])
 
 
+@pytest.mark.parametrize("hq", [0, 3, 64])
+def test_more_blocks_than_two_rounds(hq):
+    # 34 pages of 32 heads in blocks of 512 lanes, of which 512 are resident: they lie among those of the queries
+    gen = torch.Generator().manual_seed(hq)
+    page, size, heads = 64, 128, 32
+    news = [1, 130, 0, 64, 65, 33, 190, 2, 60, 61, 62, 32]
+    lengths = [9, 130, 7, 128, 200, 40, 192, 66, 64, 100, 62, 33]
+    table = _table(gen, 64, len(news), 4)
+    _step(Cache(gen, 64, heads, page, size), gen, table, news, lengths, page, torch.bfloat16, hq, heads, size, pad=1)
+
+
 def test_scales():
     """Borders of the scale (448 and just above, times powers of two), zeros, the smallest and the largest values, infinities and NaN."""
     gen = torch.Generator().manual_seed(11)
