@@ -77,12 +77,14 @@ __device__ __forceinline__ int limit_of(const Params &p, const Sequence &s, int 
 // ---- few rows: pieces of the line ----
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
 // Piece j of the line: its first unit and the one behind it, and where the first lies: the sequence and the units before it there.
-// False: beyond the line.  Up to 64 sequences are read once, a lane each (two passes over more of them).
+// False: beyond the line.  Up to 64 sequences are read once, a lane each (two passes over more of them).  The host holds the line of ascending
+// starts below 2^31 units; others may bring more (the sums stop at 2^32 - 1), and then nothing is computed.
 template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uint32_t j, uint32_t *piece, uint32_t *at, uint32_t *end, int *b, uint32_t *rest, Sequence *s,
                                            uint32_t *tiles_before, uint32_t *all_tiles) {
     const int lane = threadIdx.x & 63;
     const auto units = [&](const Sequence &q) __attribute__((always_inline)) { return tiles_of<R>(p, q) * units_of(q); };
     const auto cut = [&](uint32_t total) __attribute__((always_inline)) {
+        if (total >> 31) { *all_tiles = 0; return false; }
         const uint32_t n = (total + p.slots - 1) / p.slots;
         *piece = n < kLeast ? kLeast : n;
         *at = j * *piece;
@@ -97,7 +99,7 @@ template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uin
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const uint32_t x = __shfl_up(upto, d), y = __shfl_up(tiles_upto, d);
-            if (lane >= d) { upto += x; tiles_upto += y; }
+            if (lane >= d) { upto = __builtin_elementwise_add_sat(upto, x); tiles_upto += y; }
         }
         *all_tiles = __builtin_amdgcn_readlane(tiles_upto, 63);
         if (!cut(__builtin_amdgcn_readlane(upto, 63))) return false;
@@ -109,9 +111,9 @@ template <int R> __device__ __forceinline__ bool find_piece(const Params &p, uin
         return true;
     }
     uint32_t n = 0;
-    for (int i = lane; i < p.seq.batch; i += 64) n += units(sequence(p.seq, i));
+    for (int i = lane; i < p.seq.batch; i += 64) n = __builtin_elementwise_add_sat(n, units(sequence(p.seq, i)));
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+    for (int d = 1; d < 64; d *= 2) n = __builtin_elementwise_add_sat(n, (uint32_t)__shfl_xor(n, d));
     if (!cut(__builtin_amdgcn_readfirstlane(n)) || !locate(*at, p.seq.batch, [&](int i) __attribute__((always_inline)) -> uint32_t { return units(sequence(p.seq, i)); }, b, rest))
         return false;
     *b = __builtin_amdgcn_readfirstlane(*b);

@@ -203,6 +203,20 @@ def test_starts_that_overlap(tokens, heads, width):
     assert out.shape == q.shape
 
 
+@pytest.mark.parametrize("batch", [64, 66])
+def test_starts_that_overlap_beyond_what_is_counted(batch):
+    """Sequences of 2^30 tokens that claim all rows each: more than 2^32 pieces of work.  Nothing is computed, and nothing is joined."""
+    tokens = 6 * batch
+    q = torch.randn(tokens, 8, 64).half().cuda()
+    c = mcf.kv_cache(8, 1, 128, 64)
+    table = torch.zeros(1, 1 << 23, dtype=torch.int32, device="cuda").expand(batch, -1)
+    lengths = torch.full((batch,), 1 << 30, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, tokens] * (batch // 2) + [0], dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 3.0)
+    mcf.cache_attention(q, c, table, lengths, 0.1, starts, out=out)
+    assert (out == 3).all()
+
+
 def test_empty():
     c = mcf.kv_cache(2, 1, 16, 64)
     none = torch.zeros(0, dtype=torch.int32, device="cuda")
