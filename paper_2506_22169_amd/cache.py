@@ -3,7 +3,9 @@ Tensors go through the extension module _mcf_cache (csrc/mcf_torch_cache.cpp).
 
 Rows are [tokens, heads, size] (norm_rotate: also [batch, tokens, heads, size]), float16 or bfloat16, with a packed last
 dimension and otherwise any strides that are multiples of 8 elements, so that slices of one projection serve as they are.
-All calls are asynchronous on `stream` (None: torch's current one) and can be captured into a graph.
+All calls are asynchronous on `stream` (None: torch's current one) and can be captured into a graph.  The order of another stream behind the
+current one is the caller's to see to; the memory of what a call there reads, writes and returns is kept until both streams are through with it.
+Nothing is recorded for autograd: norm_rotate_backward is a call of its own.
 """
 from typing import NamedTuple
 

@@ -1,6 +1,8 @@
 // The calls of mcf_cache.h on torch tensors.  A CPython extension as mcf_torch.cpp is, for the same reason.
 #include "torch_call.h"
 
+#include <initializer_list>
+
 #include "../../include/mcf_cache.h"
 
 namespace mcf {
@@ -100,6 +102,31 @@ void *stream_of(PyObject *o, c10::Device device) {
     return o == Py_None ? (void *)c10::hip::getCurrentHIPStream(device.index()).stream() : PyLong_AsVoidPtr(o);
 }
 
+// The device and the stream of a call.  Where that is not torch's current stream, what the call makes is memory of its stream, and neither
+// that nor what the caller brought is handed out again before both streams are through with it.  (While the stream is captured, by whomever, no events
+// may be recorded on it: memory that a graph uses is its owner's to keep.)
+struct Place {
+    const c10::DeviceGuard on;
+    const c10::hip::HIPStream here, there;
+    const bool other;
+    Place(c10::Device device, void *stream)
+        : on(device), here(c10::hip::getCurrentHIPStream(device.index())),
+          there(here.stream() == (hipStream_t)stream ? here : c10::hip::getStreamFromExternal((hipStream_t)stream, device.index())),
+          other(here.stream() != there.stream() && !mcf::stream_capturing(there.stream())) {
+        if (other) c10::hip::setCurrentHIPStream(there);
+    }
+    ~Place() {
+        if (other) c10::hip::setCurrentHIPStream(here);
+    }
+    Place(const Place &) = delete;
+    void used(const Operands &brought, std::initializer_list<const at::Tensor *> made) const { // after the launches
+        if (!other) return;
+        for (int i = 0; i < brought.n; ++i) c10::hip::HIPCachingAllocator::recordStream(brought.all[i]->storage().data_ptr(), there);
+        for (const at::Tensor *t : made)
+            if (t->defined()) c10::hip::HIPCachingAllocator::recordStream(t->storage().data_ptr(), here);
+    }
+};
+
 void status(int st) {
     if (st == MCF_OK) return;
     static thread_local char text[512];
@@ -172,10 +199,11 @@ PyObject *norm_rotate(PyObject *const *arg, Py_ssize_t n) {
     int st;
     {
         const NoGil released;
-        const c10::DeviceGuard on(device);
+        const Place place(device, stream);
         if (!qo) { qn = like(*q); c.q_out = rows(qn); }
         if (k && !ko) { kn = like(*k); c.k_out = rows(kn); }
         st = mcf_norm_rotate(&c, stream);
+        place.used(ops, {&qn, &kn});
     }
     status(st);
     return Py_BuildValue("(NN)", wrap(qo ? *qo : qn), k ? wrap(ko ? *ko : kn) : Py_NewRef(Py_None));
@@ -210,7 +238,7 @@ PyObject *norm_rotate_backward(PyObject *const *arg, Py_ssize_t n) {
     int st;
     {
         const NoGil released;
-        const c10::DeviceGuard on(device);
+        const Place place(device, stream);
         if (!qo) { qn = like(*q); c.q_out = rows(qn); }
         if (k && !ko) { kn = like(*k); c.k_out = rows(kn); }
         const at::TensorOptions f32 = q->options().dtype(at::kFloat);
@@ -229,6 +257,7 @@ PyObject *norm_rotate_backward(PyObject *const *arg, Py_ssize_t n) {
         }
         if (st == MCF_OK) st = mcf_norm_rotate_backward(&c, ws, bytes, stream);
         if (ws) c10::hip::HIPCachingAllocator::raw_delete(ws);
+        place.used(ops, {&qn, &kn, &qw, &kw});
     }
     status(st);
     const auto or_none = [](const at::Tensor &t) { return t.defined() ? wrap(t) : Py_NewRef(Py_None); };
@@ -327,9 +356,10 @@ PyObject *append_cache(PyObject *const *arg, Py_ssize_t n) {
     int st;
     {
         const NoGil released;
-        const c10::DeviceGuard on(device);
+        const Place place(device, stream);
         if (q && !qo) { qn = like(*q); c.q_out = rows(qn); }
         st = mcf_cache_append(&c, stream);
+        place.used(ops, {&qn});
     }
     status(st);
     return q ? wrap(qo ? *qo : qn) : Py_NewRef(Py_None);
@@ -363,7 +393,7 @@ PyObject *cache_attention(PyObject *const *arg, Py_ssize_t n) {
     int st;
     {
         const NoGil released;
-        const c10::DeviceGuard on(device);
+        const Place place(device, stream);
         if (!out) { made = like(*q); c.out = rows(made); }
         int64_t bytes = 0;
         st = mcf_cache_attention_workspace(&c, &bytes);
@@ -376,6 +406,7 @@ PyObject *cache_attention(PyObject *const *arg, Py_ssize_t n) {
         }
         if (st == MCF_OK) st = mcf_cache_attention(&c, ws, ws ? bytes : 0, stream);
         if (ws) c10::hip::HIPCachingAllocator::raw_delete(ws);
+        place.used(ops, {&made});
     }
     status(st);
     return wrap(out ? *out : made);

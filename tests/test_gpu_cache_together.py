@@ -122,3 +122,59 @@ def test_training_layer():
         want, want_w, bx, bw = ref.norm_rotate_backward(dy.transpose(0, 1).cpu(), x.cpu(), layer.cos.cpu(), layer.sin.cpu(), at, w.cpu(), 1e-6, False)
         ref.check(dx, want, bx, torch.bfloat16)
         ref.check(dw, want_w, bw, torch.float32)
+
+
+@pytest.mark.parametrize("name", ["norm_rotate", "norm_rotate_backward", "append_cache", "cache_attention"])
+def test_memory_of_another_stream(name):
+    """A call on another stream while the current one, or that one, is busy: results do not lie in memory that the current stream still writes, and
+    what the call reads may be dropped right behind it."""
+    gen = torch.Generator().manual_seed(43)
+    layer = Layer(gen, torch.float16, 4, 8)
+    lengths = torch.full((4,), 100, dtype=torch.int32).cuda()
+    starts = torch.arange(5, dtype=torch.int32).cuda() * 100
+    qkv = torch.randn(400, HQ + 2 * H, D, generator=gen).half().cuda()
+    q, k, v = (t.contiguous() for t in (qkv[:, :HQ], qkv[:, HQ:HQ + H], qkv[:, HQ + H:]))
+    layer.step(qkv, lengths, starts)
+
+    def call(q, k, v, stream=None):
+        if name == "norm_rotate":
+            return mcf.norm_rotate(q, k, layer.cos, layer.sin, None, layer.wq, layer.wk, stream=stream)
+        if name == "norm_rotate_backward":
+            return mcf.norm_rotate_backward(q, k, q, k, layer.cos, layer.sin, None, layer.wq, layer.wk, stream=stream)
+        if name == "append_cache":
+            return (mcf.append_cache(layer.cache, k, v, layer.table, lengths, starts, layer.cos, layer.sin, layer.wk, q, layer.wq, stream=stream),)
+        return (mcf.cache_attention(q, layer.cache, layer.table, lengths, layer.scale, starts, stream=stream),)
+
+    want = [t.clone() for t in call(q, k, v)]
+    held = layer.held()
+
+    def same(got):  # (bytes: positions beyond the tables give NaN)
+        for a, b in zip(got, want):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+    busy, to = torch.randn(4096, 4096, device="cuda"), torch.empty(4096, 4096, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.mm(busy, busy, out=to)
+    with torch.cuda.stream(stream):
+        torch.mm(busy, busy, out=to)
+    torch.cuda.synchronize()
+    # the current stream writes memory that it has given back
+    for _ in range(20):
+        torch.mm(busy, busy, out=to)
+    for t in want:
+        torch.empty_like(t).fill_(7)
+    got = call(q, k, v, stream)
+    torch.cuda.synchronize()
+    same(got)
+    # the call's stream is behind with what it reads
+    drop = [t.clone() for t in (q, k, v)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        for _ in range(20):
+            torch.mm(busy, busy, out=to)
+    got = call(*drop, stream)
+    del drop
+    over = [torch.full_like(t, float("nan")) for t in (q, k, v)]
+    torch.cuda.synchronize()
+    same(got)
+    assert all(torch.equal(a, b) for a, b in zip(layer.held(), held)) and over[0].isnan().all()
