@@ -165,7 +165,7 @@ void norm_rotate_operands(mcf_norm_rotate_call &c, Operands &ops, const at::Tens
     if (positions) {
         if (positions->scalar_type() != at::kInt && positions->scalar_type() != at::kLong) throw Refused{MCF_EINVAL, "positions are int32 or int64"};
         const bool each = d == 4 && positions->dim() == 2;
-        if (!positions->is_contiguous() || positions->size(-1) != c.tokens || (each ? positions->size(0) != c.batch : positions->dim() != 1))
+        if (!positions->is_contiguous() || (each ? positions->size(0) != c.batch : positions->dim() != 1) || positions->size(-1) != c.tokens)
             throw Refused{MCF_EINVAL, "positions are packed, one for each token"};
         c.positions = positions->data_ptr();
         c.position_bytes = positions->scalar_type() == at::kInt ? 4 : 8;

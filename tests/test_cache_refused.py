@@ -45,6 +45,8 @@ NORM = [
     (dict(cos=z(9, 64, dtype=torch.float32)[:, ::2], sin=z(9, 64, dtype=torch.float32)[:, ::2]), EINVAL, "packed"),
     (dict(positions=torch.arange(4).float()), EINVAL, "int32 or int64"),
     (dict(positions=torch.arange(5)), EINVAL, "one for each"),
+    (dict(positions=torch.tensor(3)), EINVAL, "one for each"),
+    (dict(positions=torch.arange(4)[None]), EINVAL, "one for each"),
     (dict(positions=torch.arange(8)[::2]), EINVAL, "packed"),
     (dict(q_weight=z(32)), EINVAL, "a weight"),
     (dict(q_weight=z(64, dtype=torch.bfloat16)), EINVAL, "type of the rows"),
