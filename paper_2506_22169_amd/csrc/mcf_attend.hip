@@ -12,50 +12,75 @@ namespace mcf {
 namespace attend {
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts of a tile, for `at_once` of its rows.  A row's lanes take four
-// elements of every slices-th part each; their sums are added in that order.  Bound by latency: 4 to 6 us for the parts of 64 sequences' tiles
-// (20 MB), 8 for 5 x 8 rows of some 500 parts.
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts of a tile, for `at_once` of its rows; a lane takes four elements of a row.  One
+// row: its lanes form slices, each takes every slices-th part, and the sums are added in the slices' order.  Several: a lane takes all parts of
+// its row in order, eight asked for at once.  Bound by latency: 4 to 6 us for the parts of 64 sequences' tiles (20 MB), 8 for 5 x 8 rows of 256 parts.
 template <typename T> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
     const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once, block = blockIdx.x / groups;
     const int row0 = (int)(blockIdx.x - block * groups) * at_once, h = (int)(block % (uint32_t)p.heads);
     if (p.by_tile && block / (uint32_t)p.heads >= (uint32_t)*p.tiles) return; // (tiles < slots: the grid ends within the room for them)
     const Split t = p.splits[block];
     if (t.parts == 0 || t.rows <= row0) return;
-    const int quads = size / 4, slices = 256 / (quads * at_once);
-    const int unit = threadIdx.x / quads, slice = unit / at_once, row = at_once == 1 ? row0 : row0 + unit - slice * at_once, d = 4 * (threadIdx.x - unit * quads);
-    const bool works = slice < slices && row < t.rows;
+    const int quads = size / 4, unit = threadIdx.x / quads, d = 4 * (threadIdx.x - unit * quads), row = at_once == 1 ? row0 : row0 + unit;
     const auto at = [&](int i) __attribute__((always_inline)) {
         return ((int64_t)(i == 0 ? t.first : t.second + (i - 1) * t.step) * p.heads + h) * p.part_rows + row;
     };
+    // (a reference of -inf: nothing seen, zeros, or NaN)
+    const auto times = [](float from, float to) __attribute__((always_inline)) { return from == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(from - to); };
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    if (at_once == 1) { // one row for the whole wave
+    if (at_once == 1) {
+        const int slices = 256 / quads;
         for (int i = threadIdx.x & 63; i < t.parts; i += 64) m = fmaxf(m, p.part_ml[2 * at(i)]);
         for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-    } else if (works) {
+        if (unit < slices) {
 #pragma unroll 4
-        for (int i = 0; i < t.parts; ++i) m = fmaxf(m, p.part_ml[2 * at(i)]);
-    }
-    if (works) {
-#pragma unroll 4
-        for (int i = slice; i < t.parts; i += slices) {
-            const int64_t a = at(i);
-            const float mi = p.part_ml[2 * a], by = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - m); // (nothing seen: zeros, or NaN)
-            l += p.part_ml[2 * a + 1] * by;
-            o += *(const f32x4 *)(p.part + a * size + d) * by;
+            for (int i = unit; i < t.parts; i += slices) {
+                const int64_t a = at(i);
+                const float w = times(p.part_ml[2 * a], m);
+                l += p.part_ml[2 * a + 1] * w;
+                o += *(const f32x4 *)(p.part + a * size + d) * w;
+            }
         }
-    }
-    __shared__ f32x4 part[256];
-    __shared__ float sum[256];
-    part[threadIdx.x] = o;
-    sum[threadIdx.x] = l;
-    __syncthreads();
-    if (slice != 0 || !works) return;
-    for (int i = 1; i < slices; ++i) {
-        o += part[threadIdx.x + i * at_once * quads];
-        l += sum[threadIdx.x + i * at_once * quads];
+        __shared__ f32x4 part[256];
+        __shared__ float sum[256];
+        part[threadIdx.x] = o;
+        sum[threadIdx.x] = l;
+        __syncthreads();
+        if (unit != 0) return;
+        for (int i = 1; i < slices; ++i) {
+            o += part[threadIdx.x + i * quads];
+            l += sum[threadIdx.x + i * quads];
+        }
+    } else {
+        if (unit >= at_once || row >= t.rows) return;
+        for (int i = 0; i < t.parts; i += 8) {
+            f32x2 ml[8];
+            f32x4 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { // (behind the last part the first of them again)
+                const int64_t a = at(i + k < t.parts ? i + k : i);
+                ml[k] = *(const f32x2 *)(p.part_ml + 2 * a);
+                x[k] = *(const f32x4 *)(p.part + a * size + d);
+            }
+            float top = m;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k][0]);
+            const float by = times(m, top);
+            m = top;
+            l *= by;
+            o *= by;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (i + k >= t.parts) break;
+                const float w = times(ml[k][0], m);
+                l += ml[k][1] * w;
+                o += x[k] * w;
+            }
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     const int r = t.row + row, token = (int)quotient(r, p.group_magic, p.group_shift), head = r - token * p.group;
