@@ -34,7 +34,12 @@ template <typename T> __global__ __launch_bounds__(256) void join_kernel(const P
     float m = -INFINITY, l = 0.f;
     if (at_once == 1) {
         const int slices = 256 / quads;
-        for (int i = threadIdx.x & 63; i < t.parts; i += 64) m = fmaxf(m, p.part_ml[2 * at(i)]);
+        for (int i = threadIdx.x & 63; i < t.parts; i += 256) { // (behind the last part one of them again)
+            float x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = p.part_ml[2 * at(i + 64 * k < t.parts ? i + 64 * k : i)];
+            m = fmaxf(m, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+        }
         for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
         if (unit < slices) {
 #pragma unroll 4
