@@ -11,9 +11,9 @@
 //    columns of each of its 8 tokens (whole rows over the 16 lanes) and turns bytes in registers (v_perm); column i of
 //    product j is then column (size / 16) i + j of V, which leaves a lane with neighbouring columns of the result.
 //  - e4m3 -> 16 bit is exact; the scale of K multiplies the scores in fp32.
-// Measured: 64 sequences of up to 8192 tokens, 32 heads on 8 of 128, bf16 (529 MB), 105 us, 5.05 TB/s (a large copy: 5.15), of which the
+// Measured: 64 sequences of up to 8192 tokens, 32 heads on 8 of 128, bf16 (529 MB), 103 us, 5.1 TB/s (a large copy: 5.15), of which the
 // joining kernel is 5; with 5 rows of 8 heads each against 130000 tokens of 64 (33 MB, tiles of 48 rows) 25 us, bound by the vector instructions of
-// three products' softmax a token and the second kernel.  4 sequences of 1000 tokens: 11.8 us, of which 5 are the call; the rest are
+// three products' softmax a token and the second kernel.  4 sequences of 1000 tokens: 11.4 us, of which 5 are the call; the rest are
 // dependent loads (sequence, table, values) and the second launch.
 //
 // Weights.  V's scale is an exponent like the score's: w = 2^(s + log2 scale - m), m the running reference of these sums, and the

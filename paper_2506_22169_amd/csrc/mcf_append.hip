@@ -8,7 +8,7 @@
 // once, and K and V together keep twice the loads in flight for one search for the sequence.
 // Bound by memory with prompts (2 bytes in, 1 out an element), behind a chain of loads (the sequence, then values and page together, then
 // the scale so far) that four blocks' worth of waves a SIMD do not hide wholly: 8192 tokens of 32 + 2 x 8 heads of 128, bf16 (189 MB), 44 us,
-// 4.3 TB/s; 7 ragged prompts of 20 + 2 x 20 heads of 96 (153 MB, two of eight lanes idle) 43 us, 3.5 TB/s.  64 single tokens: 5.6 us, a launch
+// 4.3 TB/s; 7 ragged prompts of 20 + 2 x 20 heads of 96 (153 MB, two of eight lanes idle) 47 us, 3.2 TB/s.  64 single tokens: 5.6 us, a launch
 // and the chain.
 //
 // Keys are computed in 64 bits: the rounding to e4m3 is a step of 1/16 to 1/8 of a value, and a key that lies next to a border

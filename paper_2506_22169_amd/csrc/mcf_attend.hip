@@ -17,7 +17,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts of a tile, for `at_once` of its rows; a lane takes four elements of a row.  One
 // row: its lanes form slices, each takes every slices-th part, and the sums are added in the slices' order.  Several: a lane takes all parts of
-// its row in order, eight asked for at once.  Bound by latency: 4 to 6 us for the parts of 64 sequences' tiles (20 MB), 8 for 5 x 8 rows of 256 parts.
+// its row in order, eight asked for at once.  Bound by latency: 4 to 6 us for the parts of 64 sequences' tiles (20 MB), 7 for 5 x 8 rows of 256 parts.
 template <typename T> __global__ __launch_bounds__(256) void join_kernel(const Params p, int size, int at_once) {
     const uint32_t groups = (uint32_t)(p.part_rows + at_once - 1) / at_once, block = blockIdx.x / groups;
     const int row0 = (int)(blockIdx.x - block * groups) * at_once, h = (int)(block % (uint32_t)p.heads);
