@@ -89,5 +89,6 @@ def cache_attention(q, cache, table, lengths, scale, starts=None, causal=True, o
     """mcf_cache_attention: softmax(scale Q K^T) V of every row of q [tokens, q_heads, size] over the tokens of its sequence in
     `cache` (table, lengths, starts as append_cache takes them), those up to itself with causal.  Query head h reads head
     h / (q_heads / heads) of the cache.  A row that sees no token is zeros; rows outside of every sequence are left as they were
-    in `out` (and are undefined where the call makes it)."""
+    in `out` (and are undefined where the call makes it).  One kernel serves a call, by the mean number of rows: many single tokens
+    against long sequences and long prompts go faster in calls of their own."""
     return (_mod or _native()).cache_attention(q, cache, table, lengths, scale, starts, causal, out, _stream(stream))
