@@ -279,7 +279,8 @@ int plan(const mcf_norm_rotate_call *c, bool back, Plan *o) {
         o->blocks = (p.items + per_block - 1) / per_block;
         return MCF_OK;
     }
-    // one round or two of the lanes' items: as few blocks as share them evenly; more: all that are resident
+    // one round or two of the lanes' items: as few blocks as share them evenly (1500 tokens of 40 heads of 128: 16.2 us, by all that are resident
+    // 18.4, by a block an item 19.3); more: all that are resident
     const uint32_t most_q = (p.items_q + per_block - 1) / per_block, most_k = (p.items_k + per_block - 1) / per_block, most = most_q + most_k;
     const uint32_t rounds = (most + kMostBlocks - 1) / kMostBlocks;
     const auto share = [&](uint32_t n) { return rounds <= 2 ? (n + rounds - 1) / rounds : n == 0 ? 0u : n <= most / kMostBlocks ? 1u : (uint32_t)((uint64_t)kMostBlocks * n / most); };
