@@ -66,7 +66,8 @@ int mcf_norm_rotate_backward(const mcf_norm_rotate_call *call, void *workspace, 
 /*
  * The cache: keys and values as e4m3 (no infinities, NaN = 0x7f), [pages, heads, page_size, size], the last two
  * dimensions packed, element strides of the first two multiples of 16 and that of the pages below 2^32 (pointers 16-byte aligned), and an fp32 scale for
- * each page and head, [pages, heads] with a stride of its own and packed heads, not negative: the value held is e4m3 * scale.
+ * each page and head, [pages, heads] with a stride of its own and packed heads, not negative: the value held is e4m3 * scale, NaN where the
+ * scale is not finite.
  * page_size: 16, 32, 64 or 128; size: 64, 80, 96, 128, 192 or 256.
  */
 typedef struct mcf_kv_cache {

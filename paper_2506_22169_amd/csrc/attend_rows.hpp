@@ -191,7 +191,7 @@ template <typename T, int D, int NB> struct Rows {
             sv[j] = f16 ? 1.f : __uint_as_float(bits);
             f[j] = st.c * x.sk[j];
             if (f[j] < 0x1p-126f) f[j] = 0x1p-126f; // (zero would make NaN of the -inf that hides a token)
-            add[j] = x.hide[j];
+            add[j] = x.hide[j] + ((x.sk[j] - x.sk[j]) + (x.sv[j] - x.sv[j])); // (NaN for whoever sees a page whose scale is not finite)
             inv[j] = 1.f;
             if ((bits & 0x7fffff) != 0) { // no power of two
                 const float v = __uint_as_float(f16 ? bits : (bits & 0x7fffff) | 0x3f800000);
@@ -212,6 +212,12 @@ template <typename T, int D, int NB> struct Rows {
                 const v8 a = widen<T>(x.k[j][2 * c], x.k[j][2 * c + 1]);
 #pragma unroll
                 for (int n = 0; n < NB; ++n) sc[n][j] = Mma<T>::run(a, st.q[n][c], sc[n][j]);
+            }
+            if (HIDE && __any(add[j] != add[j])) { // NaN in the scores, so that rows that do not see them can be told apart
+                f[j] = sv[j] = inv[j] = 1.f;
+                add[j] = 0.f;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) sc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f} + __builtin_nanf("");
             }
         }
 #pragma unroll

@@ -201,6 +201,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             vs = *scale(p.v_scale, id, p.vs_page);
         }
     };
+    const auto not_finite = [](float x) __attribute__((always_inline)) { return (__float_as_uint(x) & 0x7f800000) == 0x7f800000; };
     const auto store = [&](uint8_t *buf, int t0) __attribute__((always_inline)) {
         const bool hides = t0 + TN > plain;
 #pragma unroll
@@ -254,7 +255,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // tokens 4t of 16 stand at 8 (t % 2) + 4 (t / 2), the order of S^T's result
             const int t = token >> 2, place = (token & ~15) + 8 * (t & 1) + 4 * ((t >> 1) & 1);
             uint8_t *const to = buf + K::k_bytes + 2 * place;
-            const float sv = K::f16 ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
+            const float sv = K::f16 || not_finite(v_scale[u]) ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
@@ -262,8 +263,10 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         if (tid < K::groups) {
             // what of V's scale is not in V goes to the exponent: all of it (fp16), or what it is beyond its power of two
             const float v = !there ? 1.f : K::f16 ? fminf(fmaxf(vs, 0x1p-60f), 0x1p60f) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
-            // (a factor of zero would make NaN of the -inf that hides a token)
-            const f32x4 x = {!there ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, there ? __builtin_amdgcn_logf(v) : -INFINITY, __builtin_amdgcn_rcpf(v), 0.f};
+            // (a factor of zero would make NaN of the -inf that hides a token; NaN for whoever sees a page whose scale is not finite)
+            const bool bad = there && (not_finite(ks) || not_finite(vs));
+            const f32x4 x = {!there || bad ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, bad ? __builtin_nanf("") : there ? __builtin_amdgcn_logf(v) : -INFINITY,
+                             __builtin_amdgcn_rcpf(v), 0.f};
             *(f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * tid) = x;
         }
     };
@@ -299,6 +302,18 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         for (int k = 0; k < K::groups; ++k) par[k] = *(const f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * k);
         if (t0 + TN > wave_all) { // (what is hidden is below everything under either sign of the scale)
             const int room = limit - t0 - 4 * g;
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < K::groups; ++k) sum += par[k][1];
+            if (__builtin_expect(__any(sum != sum), 0)) { // NaN goes to the scores, so that rows that do not see them can be told apart
+#pragma unroll
+                for (int k = 0; k < K::groups; ++k) {
+                    const bool nan = par[k][1] != par[k][1];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) sc[k / 2][8 * (k & 1) + r] = nan ? par[k][1] : sc[k / 2][8 * (k & 1) + r];
+                    par[k][1] = nan ? 0.f : par[k][1];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < K::blocks; ++j)
 #pragma unroll
