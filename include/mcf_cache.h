@@ -116,7 +116,7 @@ int mcf_cache_append(const mcf_append_call *call, void *hip_stream);
 /*
  * out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over the tokens j of the row's sequence that it sees: all of them, or
  * with causal != 0 those up to itself; query head h reads head h / (q_heads / heads) of the cache.  A row that sees no token is
- * written as zeros.  q and out are MCF_F16 or MCF_BF16; scores, weights and sums are fp32, the weights are rounded once to
+ * written as zeros, whatever its query holds; where it sees any, a query that is not finite gives NaN.  q and out are MCF_F16 or MCF_BF16; scores, weights and sums are fp32, the weights are rounded once to
  * the type of q.  What a row does not see has no effect on it, NaN included.
  * The tokens of a sequence are split over blocks where rows are few; the parts stand in the workspace and are joined in a
  * fixed order.  mcf_cache_attention_workspace: its bytes (host only); with less (NULL and 0) nothing is split.

@@ -74,6 +74,11 @@ __device__ __forceinline__ int limit_of(const Params &p, const Sequence &s, int 
     return !p.causal || n > s.seen ? s.seen : n < 0 ? 0 : n;
 }
 
+// Whether any element of a lane's query is not finite, from the largest magnitudes of both halves of its words.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 larger_halves(u16x2 most, uint32_t w) { return __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w & 0x7fff7fff)); }
+template <bool F16> __device__ __forceinline__ bool not_finite(u16x2 most) { return (most[0] > most[1] ? most[0] : most[1]) >= (F16 ? 0x7c00 : 0x7f80); }
+
 // ---- few rows: pieces of the line ----
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
 // Piece j of the line: its first unit and the one behind it, and where the first lies: the sequence and the units before it there.

@@ -23,6 +23,8 @@
 //
 // Rows see prefixes of the tokens.  What no row of the tile sees is read as zero; where only some see a token whose value is NaN
 // (0 NaN would be NaN for the others), its column's NaN are counted by a matrix product with who sees them.
+// A query that is not finite is computed as zeros, whose sum says whether it sees any token (its scores would be NaN, or all of them -inf,
+// where there is none): the check costs 0.1 us of 11.4 with 4 single tokens of 128, 0.4 of 8.2 with 7 of 256.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -336,13 +338,24 @@ template <typename T, int D, int NB, int WAVES> __device__ __forceinline__ void 
     }
     st.c = fabsf(p.c);
     const uint32_t sign = p.c < 0.f ? 0x80008000u : 0u;
+    // A query that is not finite counts as zeros until its sum is known: NaN if it sees any token.
+    bool lost[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         st.m[n] = -INFINITY;
         st.l[n] = 0.f;
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int c = 0; c < K::steps; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = larger_halves(most, q[n][c][e]);
+        uint64_t rows_lost = __ballot(not_finite<K::f16>(most));
+        rows_lost |= rows_lost >> 32;
+        rows_lost |= rows_lost >> 16;
+        lost[n] = rows_lost >> i & 1;
 #pragma unroll
         for (int c = 0; c < K::steps; ++c) {
-            const bool in = 16 * n + i < rows && (D % 32 == 0 || K::part(c, g) < D);
+            const bool in = 16 * n + i < rows && !lost[n] && (D % 32 == 0 || K::part(c, g) < D);
             st.q[n][c] = __builtin_bit_cast(typename K::v8, in ? q[n][c] ^ sign : u32x4{0, 0, 0, 0});
         }
 #pragma unroll
@@ -376,6 +389,7 @@ template <typename T, int D, int NB, int WAVES> __device__ __forceinline__ void 
     for (int n = 0; n < NB; ++n) {
         st.l[n] += __shfl_xor(st.l[n], 16);
         st.l[n] += __shfl_xor(st.l[n], 32);
+        if (lost[n] && st.l[n] != 0.f) st.l[n] = __builtin_nanf("");
         if (g == 0) { ref[wave][16 * n + i] = st.m[n]; sum[wave][16 * n + i] = st.l[n]; }
     }
     const auto top_of = [&](int r) __attribute__((always_inline)) {

@@ -137,15 +137,24 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     const int tok = token_of(real ? row : 0), head = (int)(tile * R) + (real ? row : 0) - tok * p.group;
     const int limit = real ? limit_of(p, s, tok) : s.seen;
     v8 q[K::steps];
+    bool lost; // a query that is not finite: it counts as zeros until its sum is known, and gives NaN if it sees any token
     const float c_abs = fabsf(p.c); // (a negative scale turns the queries' signs)
     const uint32_t sign = p.c < 0.f ? 0x80008000u : 0u;
     {
         const T *src = (const T *)p.q + (int64_t)(s.first + tok) * p.qt + (int64_t)(h * p.group + head) * p.qh + 8 * g;
+        u16x2 most = {0, 0};
+        u32x4 w[K::steps];
 #pragma unroll
         for (int c = 0; c < K::steps; ++c) {
-            const u32x4 w = *(const u32x4 *)(src + 16 * c);
-            q[c] = __builtin_bit_cast(v8, real ? w ^ sign : u32x4{0, 0, 0, 0});
+            w[c] = *(const u32x4 *)(src + 16 * c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = larger_halves(most, w[c][e]);
         }
+        uint64_t rows_lost = __ballot(not_finite<K::f16>(most));
+        rows_lost |= rows_lost >> 32;
+        lost = rows_lost >> i & 1;
+#pragma unroll
+        for (int c = 0; c < K::steps; ++c) q[c] = __builtin_bit_cast(v8, real && !lost ? w[c] ^ sign : u32x4{0, 0, 0, 0});
     }
     for (int d = tid; d < D; d += K::threads) first_nan[d] = 0x7fffffff;
 
@@ -201,7 +210,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             vs = *scale(p.v_scale, id, p.vs_page);
         }
     };
-    const auto not_finite = [](float x) __attribute__((always_inline)) { return (__float_as_uint(x) & 0x7f800000) == 0x7f800000; };
+    const auto scale_lost = [](float x) __attribute__((always_inline)) { return (__float_as_uint(x) & 0x7f800000) == 0x7f800000; };
     const auto store = [&](uint8_t *buf, int t0) __attribute__((always_inline)) {
         const bool hides = t0 + TN > plain;
 #pragma unroll
@@ -255,7 +264,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // tokens 4t of 16 stand at 8 (t % 2) + 4 (t / 2), the order of S^T's result
             const int t = token >> 2, place = (token & ~15) + 8 * (t & 1) + 4 * ((t >> 1) & 1);
             uint8_t *const to = buf + K::k_bytes + 2 * place;
-            const float sv = K::f16 || not_finite(v_scale[u]) ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
+            const float sv = K::f16 || scale_lost(v_scale[u]) ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
@@ -264,7 +273,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // what of V's scale is not in V goes to the exponent: all of it (fp16), or what it is beyond its power of two
             const float v = !there ? 1.f : K::f16 ? fminf(fmaxf(vs, 0x1p-60f), 0x1p60f) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
             // (a factor of zero would make NaN of the -inf that hides a token; NaN for whoever sees a page whose scale is not finite)
-            const bool bad = there && (not_finite(ks) || not_finite(vs));
+            const bool bad = there && (scale_lost(ks) || scale_lost(vs));
             const f32x4 x = {!there || bad ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, bad ? __builtin_nanf("") : there ? __builtin_amdgcn_logf(v) : -INFINITY,
                              __builtin_amdgcn_rcpf(v), 0.f};
             *(f32x4 *)(buf + K::k_bytes + K::v_bytes + 16 * tid) = x;
@@ -387,6 +396,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
     // ---- the result ----
     l += __shfl_xor(l, 32);
     if (!real) return;
+    if (lost && l != 0.f) l = __builtin_nanf("");
     const bool whole = chunks == 1;
     const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.0f / l;
     const int64_t place = ((int64_t)slot * p.heads + h) * p.part_rows + row;
