@@ -79,6 +79,10 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u16x2 larger_halves(u16x2 most, uint32_t w) { return __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w & 0x7fff7fff)); }
 template <bool F16> __device__ __forceinline__ bool not_finite(u16x2 most) { return (most[0] > most[1] ? most[0] : most[1]) >= (F16 ? 0x7c00 : 0x7f80); }
 
+// V's scale as fp16 weights carry it (in their exponent).  From below: fp16 results cannot tell values under 448 * 2^-60 from zeros, and a weight of more
+// range would leave the sum of the softmax nothing of such tokens.  From above: its reciprocal stays a normal number.
+__device__ __forceinline__ float scale_of_weights(float scale) { return fminf(fmaxf(scale, 0x1p-60f), 0x1p126f); }
+
 // ---- few rows: pieces of the line ----
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }
 // Piece j of the line: its first unit and the one behind it, and where the first lies: the sequence and the units before it there.

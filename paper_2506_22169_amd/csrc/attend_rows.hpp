@@ -189,7 +189,7 @@ template <typename T, int D, int NB> struct Rows {
         float f[2], add[2], inv[2], sv[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(f16 ? fminf(fmaxf(x.sv[j], 0x1p-60f), 0x1p60f) : x.sv[j]));
+            const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(f16 ? scale_of_weights(x.sv[j]) : x.sv[j]));
             sv[j] = f16 ? 1.f : __uint_as_float(bits);
             f[j] = st.c * x.sk[j];
             if (f[j] < 0x1p-126f) f[j] = 0x1p-126f; // (zero would make NaN of the -inf that hides a token)

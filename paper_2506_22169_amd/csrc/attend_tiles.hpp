@@ -271,7 +271,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
         }
         if (tid < K::groups) {
             // what of V's scale is not in V goes to the exponent: all of it (fp16), or what it is beyond its power of two
-            const float v = !there ? 1.f : K::f16 ? fminf(fmaxf(vs, 0x1p-60f), 0x1p60f) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
+            const float v = !there ? 1.f : K::f16 ? scale_of_weights(vs) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
             // (a factor of zero would make NaN of the -inf that hides a token; NaN for whoever sees a page whose scale is not finite)
             const bool bad = there && (scale_lost(ks) || scale_lost(vs));
             const f32x4 x = {!there || bad ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, bad ? __builtin_nanf("") : there ? __builtin_amdgcn_logf(v) : -INFINITY,
