@@ -79,9 +79,19 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u16x2 larger_halves(u16x2 most, uint32_t w) { return __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w & 0x7fff7fff)); }
 template <bool F16> __device__ __forceinline__ bool not_finite(u16x2 most) { return (most[0] > most[1] ? most[0] : most[1]) >= (F16 ? 0x7c00 : 0x7f80); }
 
-// V's scale as fp16 weights carry it (in their exponent).  From below: fp16 results cannot tell values under 448 * 2^-60 from zeros, and a weight of more
-// range would leave the sum of the softmax nothing of such tokens.  From above: its reciprocal stays a normal number.
-__device__ __forceinline__ float scale_of_weights(float scale) { return fminf(fmaxf(scale, 0x1p-60f), 0x1p126f); }
+// V's scale (its bits) in two factors: a power of two that goes into V as it is widened, and the rest, which the weights have in their exponent.
+// bf16 takes any power of two, fp16 those under which e4m3 stays exact (2^-9 to 448): 2^-15 to 2^7.  Rests of fp16 are held to 2^-45, where results cannot
+// tell the values from zeros (448 * 2^-60; a weight of more range would leave the sum of the softmax nothing of such tokens), and to 2^119, whose
+// reciprocal is still a normal number.  Scales that are not finite give any rest.
+template <bool F16> __device__ __forceinline__ uint32_t scale_in_v(uint32_t scale) {
+    const uint32_t power = scale & 0x7f800000, low = 0x38000000, high = 0x43000000;
+    return !F16 ? power : power < low ? low : power < high ? power : high;
+}
+template <bool F16> __device__ __forceinline__ uint32_t scale_in_weights(uint32_t scale) {
+    if (!F16) return (scale & 0x7fffff) | 0x3f800000;
+    const uint32_t held = scale < 0x21800000 ? 0x21800000 : scale < 0x7e800000 ? scale : 0x7e800000; // 2^-60, 2^126
+    return held - scale_in_v<true>(held) + 0x3f800000;
+}
 
 // ---- few rows: pieces of the line ----
 __device__ __forceinline__ uint32_t units_of(const Sequence &s) { return (uint32_t)(s.seen + kUnit - 1) / kUnit + 1; }

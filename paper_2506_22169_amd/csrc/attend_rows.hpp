@@ -16,10 +16,10 @@
 // three products' softmax a token and the second kernel.  4 sequences of 1000 tokens: 11.4 us, of which 5 are the call; the rest are
 // dependent loads (sequence, table, values) and the second launch.
 //
-// Weights.  V's scale is an exponent like the score's: w = 2^(s + log2 scale - m), m the running reference of these sums, and the
-// sum of the softmax adds w / scale; the largest weight stands near 1 whatever the scales, where fp16 has all its bits.  For bf16
-// (with fp32's range) the power of two of the scale is in V instead, where the widening instruction takes it, and only the rest of it in
-// the exponent.  Each weight is rounded once.  The reference moves only when a score outgrows it by 2^8.  Scales of K are not negative.
+// Weights.  The power of two of V's scale is in V, where the widening instruction takes it; what is left of the scale (its mantissa; fp16: also what is
+// beyond the powers that its range holds) is an exponent like the score's: w = 2^(s + log2 rest - m), m the running reference of these sums,
+// and the sum of the softmax adds w / rest.  So the largest weight stands near 1, and pages under scales far apart have weights of all bits beside one another.
+// Each weight is rounded once.  The reference moves only when a score outgrows it by 2^8.  Scales of K are not negative.
 //
 // Rows see prefixes of the tokens.  What no row of the tile sees is read as zero; where only some see a token whose value is NaN
 // (0 NaN would be NaN for the others), its column's NaN are counted by a matrix product with who sees them.
@@ -185,23 +185,22 @@ template <typename T, int D, int NB> struct Rows {
     template <bool HIDE> static __device__ __forceinline__ void step(const Params &p, Step<D> &x, int t, int end, int all, State &st) {
         const int lane = threadIdx.x & 63, g = lane >> 4;
         v8 pw[NB];
-        // factor and addend of the scores, and what V's scale put into the exponent: all of it (fp16), or what is beyond its power of two
+        // factor and addend of the scores, V's factor, and the reciprocal of what V's scale has in the weights
         float f[2], add[2], inv[2], sv[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(f16 ? scale_of_weights(x.sv[j]) : x.sv[j]));
-            sv[j] = f16 ? 1.f : __uint_as_float(bits);
+            const uint32_t bits = __builtin_amdgcn_readfirstlane(__float_as_uint(x.sv[j])), rest = scale_in_weights<f16>(bits);
+            sv[j] = __uint_as_float(scale_in_v<f16>(bits));
             f[j] = st.c * x.sk[j];
             if (f[j] < 0x1p-126f) f[j] = 0x1p-126f; // (zero would make NaN of the -inf that hides a token)
             add[j] = x.hide[j] + ((x.sk[j] - x.sk[j]) + (x.sv[j] - x.sv[j])); // (NaN for whoever sees a page whose scale is not finite)
             inv[j] = 1.f;
-            if ((bits & 0x7fffff) != 0) { // no power of two
-                const float v = __uint_as_float(f16 ? bits : (bits & 0x7fffff) | 0x3f800000);
-                add[j] += __builtin_amdgcn_logf(v);
-                inv[j] = __builtin_amdgcn_rcpf(v);
+            if ((rest & 0x7fffff) != 0) { // no power of two
+                add[j] += __builtin_amdgcn_logf(__uint_as_float(rest));
+                inv[j] = __builtin_amdgcn_rcpf(__uint_as_float(rest));
             } else if (f16) {
-                add[j] += (float)((int)(bits >> 23) - 127);
-                inv[j] = __uint_as_float((254 - (bits >> 23)) << 23);
+                add[j] += (float)((int)(rest >> 23) - 127);
+                inv[j] = __uint_as_float((254 - (rest >> 23)) << 23);
             }
         }
         f32x4 sc[NB][2];

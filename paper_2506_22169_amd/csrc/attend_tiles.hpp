@@ -5,7 +5,7 @@
 //     and S^T's result layout is P^T's operand as it is, with the tokens counted in that order.
 // Bound by the matrix instructions and, next to them, by the vector instructions of the softmax and the LDS reads of their
 // operands.  Therefore
-//  - K and V are widened from e4m3 once for a block (exactly; bf16: with the power of two of V's scale on the way) while they go
+//  - K and V are widened from e4m3 once for a block (exactly; V with the power of two of its scale on the way) while they go
 //    from registers to LDS, K as rows, V transposed, so that every operand is one 128-bit read; two tiles of LDS in turn, one
 //    barrier a tile, the loads of the tile after next in flight meanwhile.
 //  - V is transposed by bytes before it is widened: a lane has 4 tokens of 4 neighbouring columns.  Which column is which row of
@@ -201,7 +201,7 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             const uint8_t *v = page(v_head, vi, p.v_page) + (((t0 + v_token[u]) & in_page) * D + v_at[u]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) vw[u][r] = *(const uint32_t *)(v + r * D);
-            if (!K::f16) v_scale[u] = *scale(p.v_scale, vi, p.vs_page);
+            v_scale[u] = *scale(p.v_scale, vi, p.vs_page);
         }
         if (tid < K::groups) {
             there = valid(t0 + 16 * tid, g_id);
@@ -264,14 +264,13 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES)
             // tokens 4t of 16 stand at 8 (t % 2) + 4 (t / 2), the order of S^T's result
             const int t = token >> 2, place = (token & ~15) + 8 * (t & 1) + 4 * ((t >> 1) & 1);
             uint8_t *const to = buf + K::k_bytes + 2 * place;
-            const float sv = K::f16 || scale_lost(v_scale[u]) ? 1.f : v_scale[u]; // (of which the instruction takes the power of two)
+            const float sv = !K::f16 && scale_lost(v_scale[u]) ? 1.f : __uint_as_float(scale_in_v<K::f16>(__float_as_uint(v_scale[u])));
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 *(u32x2 *)(to + Columns<D>::row(c, e) * K::v_pitch) = u32x2{Wide<T>::template two<false>(y[e], sv), Wide<T>::template two<true>(y[e], sv)};
         }
         if (tid < K::groups) {
-            // what of V's scale is not in V goes to the exponent: all of it (fp16), or what it is beyond its power of two
-            const float v = !there ? 1.f : K::f16 ? scale_of_weights(vs) : __uint_as_float((__float_as_uint(vs) & 0x7fffff) | 0x3f800000);
+            const float v = !there ? 1.f : __uint_as_float(scale_in_weights<K::f16>(__float_as_uint(vs)));
             // (a factor of zero would make NaN of the -inf that hides a token; NaN for whoever sees a page whose scale is not finite)
             const bool bad = there && (scale_lost(ks) || scale_lost(vs));
             const f32x4 x = {!there || bad ? 1.f : ks * c_abs < 0x1p-126f ? 0x1p-126f : ks * c_abs, bad ? __builtin_nanf("") : there ? __builtin_amdgcn_logf(v) : -INFINITY,
