@@ -5,13 +5,14 @@ Rows are [tokens, heads, size] (norm_rotate: also [batch, tokens, heads, size]),
 dimension and otherwise any strides that are multiples of 8 elements, so that slices of one projection serve as they are.
 All calls are asynchronous on `stream` (None: torch's current one) and can be captured into a graph.  The order of another stream behind the
 current one is the caller's to see to; the memory of what a call there reads, writes and returns is kept until both streams are through with it.
-Nothing is recorded for autograd: norm_rotate_backward is a call of its own.
+norm_rotate is recorded for autograd where its operands ask for it; append_cache and cache_attention are not, their results have no gradients.
 """
 from typing import NamedTuple
 
 from .binding import McfError, _stream_ptr, load_library
 
 _mod = None
+_function = None  # norm_rotate for autograd
 
 
 class KVCache(NamedTuple):
@@ -56,8 +57,45 @@ def norm_rotate(q, k=None, cos=None, sin=None, positions=None, q_weight=None, k_
     row of cos and sin (float32 [positions, rotary / 2]; None: none) that its position names, in one pass.
     positions: int32 or int64 [tokens] or [batch, tokens]; None counts the tokens of a batch row from 0; one outside of
     the tables gives NaN.  The pairs are (j, j + rotary / 2), or (2j, 2j + 1) with interleaved.  Returns (q_out, k_out), None
-    without k; the outputs may be q and k themselves."""
-    return (_mod or _native()).norm_rotate(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, _stream(stream))
+    without k; the outputs may be q and k themselves.
+    Where q, k or a weight requires a gradient and torch records, the gradients are norm_rotate_backward's, which autograd runs on the stream that was
+    torch's current one.  Such a call is refused with q_out or k_out and while its stream is captured: a captured training step calls
+    norm_rotate under torch.no_grad() and norm_rotate_backward itself."""
+    out = (_mod or _native()).norm_rotate(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, _stream(stream))
+    return out if out is not NotImplemented else _recorded().apply(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, stream)
+
+
+def _recorded():
+    """norm_rotate as a function of autograd's."""
+    global _function
+    if _function is None:
+        import torch
+
+        class NormRotate(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, stream):
+                ctx.save_for_backward(q, k, q_weight, k_weight, cos, sin, positions)
+                ctx.rest = eps, interleaved
+                return _native().norm_rotate(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, None, None, _stream(stream))
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, dq, dk):
+                q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
+                if torch.cuda.is_current_stream_capturing():  # (autograd's own streams beside the captured one can end the process)
+                    raise McfError(2, "recorded gradients are not captured: norm_rotate_backward is")
+                dq, dk = (t if t is None or _laid_out(t) else t.contiguous() for t in (dq, dk))  # (the gradient of a sum is one number, expanded)
+                gq, gk, gqw, gkw = norm_rotate_backward(dq, dk, q, k, cos, sin, positions, q_weight, k_weight, *ctx.rest)
+                gqw, gkw = (g if g is None else g.to(w.dtype) for g, w in ((gqw, q_weight), (gkw, k_weight)))
+                return gq, gk, gqw, gkw, None, None, None, None, None, None
+
+        _function = NormRotate
+    return _function
+
+
+def _laid_out(t):
+    """Whether rows have a layout that the calls take."""
+    return t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(s % 8 == 0 for s, n in zip(t.stride()[:-1], t.shape) if n > 1)
 
 
 def norm_rotate_backward(dq, dk, q, k=None, cos=None, sin=None, positions=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,

@@ -1,6 +1,9 @@
 // The calls of mcf_cache.h on torch tensors.  A CPython extension as mcf_torch.cpp is, for the same reason.
 #include "torch_call.h"
 
+#include <ATen/core/grad_mode.h>
+
+#include <algorithm>
 #include <initializer_list>
 
 #include "../../include/mcf_cache.h"
@@ -176,7 +179,17 @@ void norm_rotate_operands(mcf_norm_rotate_call &c, Operands &ops, const at::Tens
     if (PyErr_Occurred()) throw Refused{0, nullptr};
 }
 
-// norm_rotate(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, stream) -> (q_out, k_out)
+// Whether a call is to be recorded for autograd, which Python does (NotImplemented): into new tensors, outside of captures.
+bool recorded(std::initializer_list<const at::Tensor *> operands, std::initializer_list<const at::Tensor *> tables, bool results_given) {
+    const auto wanted = [](const at::Tensor *t) { return t && t->requires_grad(); };
+    if (!at::GradMode::is_enabled()) return false;
+    if (std::any_of(tables.begin(), tables.end(), wanted)) throw Refused{MCF_EUNSUPPORTED, "the tables have no gradients"};
+    if (std::none_of(operands.begin(), operands.end(), wanted)) return false;
+    if (results_given) throw Refused{MCF_EUNSUPPORTED, "results in tensors of the caller are not recorded for autograd (torch.no_grad() and norm_rotate_backward)"};
+    return true;
+}
+
+// norm_rotate(q, k, cos, sin, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, stream) -> (q_out, k_out), or NotImplemented: to be recorded
 PyObject *norm_rotate(PyObject *const *arg, Py_ssize_t n) {
     if (n != 12) return PyErr_Format(PyExc_TypeError, "norm_rotate takes 12 arguments");
     const at::Tensor *q = tensor(arg[0], "q is missing"), *k = tensor(arg[1], nullptr), *qo = tensor(arg[9], nullptr), *ko = tensor(arg[10], nullptr);
@@ -193,9 +206,15 @@ PyObject *norm_rotate(PyObject *const *arg, Py_ssize_t n) {
     c.q_out = qo ? rows(*qo) : packed_q;
     if (k) c.k_out = ko ? rows(*ko) : mcf_rows{k->data_ptr(), {c.tokens * c.k_heads * c.size, c.k_heads * c.size, c.size}};
     status(mcf::check_norm_rotate(&c, false));
+    const bool record = recorded({q, k, tensor(arg[5], nullptr), tensor(arg[6], nullptr)}, {tensor(arg[2], nullptr), tensor(arg[3], nullptr)}, qo || ko);
     const c10::Device device = ops.device();
     void *stream = stream_of(arg[11], device);
     if (PyErr_Occurred()) return nullptr;
+    if (record) {
+        if (mcf::stream_capturing(stream))
+            throw Refused{MCF_EUNSUPPORTED, "a call that is captured is not recorded for autograd (torch.no_grad() and norm_rotate_backward)"};
+        return Py_NewRef(Py_NotImplemented);
+    }
     int st;
     {
         const NoGil released;
