@@ -80,7 +80,8 @@ typedef struct mcf_kv_cache {
 
 /*
  * The sequences of a call: rows starts[b] .. starts[b + 1] - 1 of the call's token tensors belong to sequence b (starts
- * NULL: one row each, row b); rows outside of every sequence are neither read nor written.  lengths[b] counts the tokens of the
+ * NULL: one row each, row b); rows outside of every sequence are not written, and what they hold has no effect.  Starts ascend: with others, rows that
+ * several sequences claim get the result of any of them, and rows may be left out.  lengths[b] counts the tokens of the
  * sequence, those rows the last of them: row i of n is token lengths[b] - n + i.  Token t is held in place
  * t % page_size of page table[b][t / page_size] (`table_width` columns; stride in elements).  A token whose page number
  * is outside of the cache, or that is beyond the table, is not there: nothing is written for it and nobody sees it.
@@ -94,8 +95,8 @@ typedef struct mcf_sequences {
 
 /*
  * k and v [tokens, heads, size] (mcf_rows with the batch stride unused) go into the cache.  Keys get mcf_norm_rotate's norm
- * (k_weight) and rotation (tables) first, with the token's place in its sequence as the position, in 64 bits up to the
- * rounding to e4m3.  The scale of a page and head is the least power of two, 2^-100 at least, that brings its largest
+ * (k_weight) and rotation (tables) first, with the token's place in its sequence as the position, in 64 bits, rounded
+ * to fp32 and then to e4m3.  The scale of a page and head is the least power of two, 2^-100 at least, that brings its largest
  * finite value to 448 at most; where a page holds earlier tokens of the sequence, its scale only grows, and they are
  * rounded again when it does.  (Scales are powers of two because e4m3 then loses nothing by them but what falls below
  * its smallest exponent.)  Values that are not finite are held as NaN.  A page that is written belongs to one sequence.
@@ -117,7 +118,7 @@ int mcf_cache_append(const mcf_append_call *call, void *hip_stream);
  * out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over the tokens j of the row's sequence that it sees: all of them, or
  * with causal != 0 those up to itself; query head h reads head h / (q_heads / heads) of the cache.  A row that sees no token is
  * written as zeros, whatever its query holds; where it sees any, a query that is not finite gives NaN.  q and out are MCF_F16 or MCF_BF16; scores, weights and sums are fp32, the weights are rounded once to
- * the type of q.  What a row does not see has no effect on it, NaN included.
+ * the type of q.  (fp16: scales of V below 2^-60 count as 2^-60, which no fp16 result can tell, above 2^126 as 2^126.)  What a row does not see has no effect on it, NaN included.
  * The tokens of a sequence are split over blocks where rows are few; the parts stand in the workspace and are joined in a
  * fixed order.  mcf_cache_attention_workspace: its bytes (host only); with less (NULL and 0) nothing is split.
  */

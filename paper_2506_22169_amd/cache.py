@@ -114,7 +114,7 @@ def append_cache(cache, k, v, table, lengths, starts=None, cos=None, sin=None, k
 
     table int32 [sequences, pages]: the pages of each sequence (a number outside of the cache: no page); lengths int32
     [sequences]: its tokens, the new ones the last of them; starts int32 [sequences + 1]: whose rows are whose
-    (starts[b] .. starts[b + 1] - 1; None: one row each).  Rows outside of every sequence are left alone.
+    (starts[b] .. starts[b + 1] - 1, ascending; None: one row each).  Rows outside of every sequence are left alone.
     The scale of a page and head is a power of two from its largest value; in a page that holds earlier tokens it only
     grows, and those are rounded again when it does.  A page that is written belongs to one sequence.
     q [tokens, q_heads, size], q_weight: the queries of the same tokens get their norm and rotation in the same launch; returns
@@ -127,6 +127,6 @@ def cache_attention(q, cache, table, lengths, scale, starts=None, causal=True, o
     """mcf_cache_attention: softmax(scale Q K^T) V of every row of q [tokens, q_heads, size] over the tokens of its sequence in
     `cache` (table, lengths, starts as append_cache takes them), those up to itself with causal.  Query head h reads head
     h / (q_heads / heads) of the cache.  A row that sees no token is zeros; rows outside of every sequence are left as they were
-    in `out` (and are undefined where the call makes it).  One kernel serves a call, by the mean number of rows: many single tokens
-    against long sequences and long prompts go faster in calls of their own."""
+    in `out` (and are undefined where the call makes it).  One kernel serves a call, by the mean number of rows: single tokens
+    against long sequences and long prompts go faster in calls of their own (up to six times: 8 tokens against 130000 beside a prompt of 512)."""
     return (_mod or _native()).cache_attention(q, cache, table, lengths, scale, starts, causal, out, _stream(stream))

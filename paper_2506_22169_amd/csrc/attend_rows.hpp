@@ -11,9 +11,10 @@
 //    columns of each of its 8 tokens (whole rows over the 16 lanes) and turns bytes in registers (v_perm); column i of
 //    product j is then column (size / 16) i + j of V, which leaves a lane with neighbouring columns of the result.
 //  - e4m3 -> 16 bit is exact; the scale of K multiplies the scores in fp32.
-// Measured: 64 sequences of up to 8192 tokens, 32 heads on 8 of 128, bf16 (529 MB), 103 us, 5.1 TB/s (a large copy: 5.15), of which the
-// joining kernel is 5; with 5 rows of 8 heads each against 130000 tokens of 64 (33 MB, tiles of 48 rows) 25 us, bound by the vector instructions of
-// three products' softmax a token and the second kernel.  4 sequences of 1000 tokens: 11.4 us, of which 5 are the call; the rest are
+// Measured: 64 sequences of up to 8192 tokens, 32 heads on 8 of 128, bf16 (529 MB), 104 us, 5.1 TB/s (a large copy: 5.15), of which the
+// joining kernel is 5; with 5 rows of 8 heads each against 130000 tokens of 64 (33 MB, tiles of 48 rows) 25 us, of which 14 are what 1000 tokens take (two
+// launches, their chains of loads, 256 parts a tile to join) and another 130000 tokens are 7, 4.6 TB/s; vector instructions take 53 % of the SIMDs' cycles
+// and waves wait for 42 % of theirs.  4 sequences of 1000 tokens: 11.5 us, of which 5 are the call; the rest are
 // dependent loads (sequence, table, values) and the second launch.
 //
 // Weights.  The power of two of V's scale is in V, where the widening instruction takes it; what is left of the scale (its mantissa; fp16: also what is

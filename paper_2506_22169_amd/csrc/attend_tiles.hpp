@@ -12,10 +12,10 @@
 //    an operand is free; the order taken (Columns) spreads the writes over the banks and leaves a lane with up to 16
 //    neighbouring columns of the result.
 //  - Padding of 16 bytes a row puts the rows of both on different banks.
-// Measured: 4096 tokens of 32 heads on 8 of 128 behind 12288 (9.6e11 flop over the visible pairs), bf16, 885 to 920 us, 1.05 to 1.09 PFLOP/s (a large matrix product:
-// 1.40).  With parts left out, each alone: without staging 130 us less, without the LDS reads of operands 130 to 170, without the exponentials
-// 75; the matrix instructions alone are some 550.  7 ragged prompts of up to 1500 tokens behind up to 100, 20 heads of 80, fp16: 66 us, 0.34 PFLOP/s:
-// 580 blocks of 1 to 13 steps on 256 units, rows of 80 padded to 96 for V's product, masked halves of the tiles at the diagonal.
+// Measured: 4096 tokens of 32 heads on 8 of 128 behind 12288 (9.6e11 flop over the visible pairs), bf16, 885 to 960 us by the card, up to 1.09 PFLOP/s (a large matrix product:
+// 1.34 to 1.40).  With parts left out, each alone: without staging 130 us less, without the LDS reads of operands 130 to 170, without the exponentials
+// 75; the matrix instructions alone are some 550.  7 ragged prompts of up to 1500 tokens behind up to 100, 20 heads of 80, fp16: 67 us, 0.33 PFLOP/s:
+// 580 blocks of 1 to 13 steps, one at a time on each of 256 units, whose begin and end nothing covers: waves wait for 46 % of their time.
 //
 // Weights and what rows do not see: as in attend_rows.hpp.  A NaN in V that only some
 // rows of the tile see is taken out and its first token noted for its column; rows that see that token get NaN.

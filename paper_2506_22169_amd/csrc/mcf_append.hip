@@ -6,15 +6,15 @@
 // are held) concerns nobody else, so there are no atomics and the result does not depend on any order.  Its lanes keep
 // the page's new values in registers between the search for the largest and the rounding, so that the inputs are read
 // once, and K and V together keep twice the loads in flight for one search for the sequence.
-// Bound by memory with prompts (2 bytes in, 1 out an element), behind a chain of loads (the sequence, then values and page together, then
-// the scale so far) that four blocks' worth of waves a SIMD do not hide wholly: 8192 tokens of 32 + 2 x 8 heads of 128, bf16 (189 MB), 44 us,
-// 4.3 TB/s; 7 ragged prompts of 20 + 2 x 20 heads of 96 (153 MB, two of eight lanes idle) 47 us, 3.2 TB/s.  64 single tokens: 5.6 us, a launch
-// and the chain.
+// With prompts the bytes (2 in, 1 out an element) and the vector instructions (keys, the largest value, rounding) take about as long, behind a chain of
+// loads (the sequence, then values and page together, then the scale so far): 8192 tokens of 32 + 2 x 8 heads of 128, bf16 (189 MB), 42 us, with
+// a norm 44, 4.3 TB/s; 7 ragged prompts of 20 + 2 x 20 heads of 96 (153 MB, two of eight lanes idle) 47 us, with a norm 53, vector instructions in
+// 82 % of the SIMDs' cycles.  64 single tokens: 5.6 us, a launch and the chain.
 //
 // Keys are computed in 64 bits: the rounding to e4m3 is a step of 1/16 to 1/8 of a value, and a key that lies next to a border
-// between two steps would otherwise go to either side by the order of the sums, so that the same token appended alone and
-// within a prompt could be held as two values.  A row takes about 150 double operations a lane, behind its loads: in 32 bits the prompts above
-// would take 1 to 2 us less (46.4 -> 45.4, 46.6 -> 44.4 when measured; with a norm 51.4 -> 46.5).
+// between two steps would in 32 bits go to either side by a rounding of its norm, a whole step from the nearest to the definition's value.  (The order of a
+// row's sums is its size's alone: a token appended alone and within a prompt gives the same bits either way.)  A row takes about 150 double
+// operations a lane.  In 32 bits the calls above would take 41.8 (42.0 in 64), 42.4 (44.4), 44.4 (46.9) and 47.4 us (52.7).
 #include <hip/hip_runtime.h>
 
 #include <initializer_list>
