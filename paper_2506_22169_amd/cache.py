@@ -118,7 +118,7 @@ def append_cache(cache, k, v, table, lengths, starts=None, cos=None, sin=None, k
     The scale of a page and head is a power of two from its largest value; in a page that holds earlier tokens it only
     grows, and those are rounded again when it does.  A page that is written belongs to one sequence.
     q [tokens, q_heads, size], q_weight: the queries of the same tokens get their norm and rotation in the same launch; returns
-    q_out (may be q), None without q."""
+    q_out (may be q; rows outside of every sequence are undefined where the call makes it), None without q."""
     return (_mod or _native()).append_cache(cache, k, v, table, lengths, starts, cos, sin, k_weight, q, q_weight, eps, interleaved, q_out,
                                             _stream(stream))
 
